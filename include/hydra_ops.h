@@ -145,6 +145,71 @@ int hydra_op_embed_bwd(int dtype, int V, int S, int S_table, int B, int d, int l
                        const int32_t* positions, const void* const* dx, float* const* dtok, float* const* dpos,
                        void* stream);
 
+/* ---- A decoder's next tokens: keys and values in a paged cache of 8-bit codes, attention over it, drawing a token -----------------
+ *
+ * The cache of one layer of each of G models.  A pool k_g (and v_g) has n_pages pages, page_bytes from one to the next; a page is
+ * [HKV, page, DH] codes of one byte, its scale of head h is k_scale_g[p*HKV + h], and a code stands for code * scale.  HYDRA_CACHE_INT8:
+ * -127..127; HYDRA_CACHE_E4M3: 1 sign, 4 exponent, 3 fraction bits, largest 448, no infinities.  Tokens [i*page, (i+1)*page) of sequence b
+ * lie in page page_table[b*max_pages + i] of every model's pool; entries past its last page are not used, and a page id outside [0, n_pages)
+ * holds nothing: nothing is stored there, and its tokens are masked.
+ * lens[b]: tokens of sequence b with those of the call; the call's n tokens of b are the last n of them, at positions lens[b]-n .. lens[b]-1, and
+ * are rows q_ptr[b] .. q_ptr[b+1]-1 of the call's matrices.  q_ptr NULL: one token per sequence, row b.  A sequence may have no tokens in a call,
+ * and no tokens at all.  The host's bounds: n_tok = q_ptr[B] rows, max_q rows of one sequence, max_len tokens in one (at most
+ * max_pages*page); the kernels hold what the device arrays say to these bounds.  page_table, lens and q_ptr are device arrays that the
+ * group shares.  page 16, 32, 64 or 128; DH 64 or 128; pools 16-byte aligned, page_bytes 0 (HKV*page*DH) or a multiple of 16 of at
+ * least that, for pools that several layers or k and v share. */
+enum { HYDRA_CACHE_INT8 = 0, HYDRA_CACHE_E4M3 = 1 };
+enum { HYDRA_ROT_NONE = 0, HYDRA_ROT_HALVES = 1, HYDRA_ROT_NEIGHBOURS = 2 };
+typedef struct {
+  int kind, B, HKV, DH, page, n_pages, max_pages, G;
+  int n_tok, max_q, max_len;
+  size_t page_bytes;
+  const int32_t* page_table;
+  const int32_t* lens;
+  const int32_t* q_ptr;
+  void* const* k;
+  void* const* v;
+  float* const* k_scale;
+  float* const* v_scale;
+} hydra_cache_desc;
+
+/* The call's keys and values into the cache.  qkv_g [n_tok, ld_qkv] bf16: H query heads of DH columns, then HKV key heads, then HKV value heads;
+ * 16-byte aligned, ld_qkv a multiple of 8.  The position rotation turns the first rot_dim columns (a multiple of 16) of every query and key head:
+ * with c, s = cos_sin[position*rot_dim + i], cos_sin[position*rot_dim + rot_dim/2 + i] and a, b = columns i and i + rot_dim/2
+ * (HYDRA_ROT_HALVES) or 2i and 2i + 1 (HYDRA_ROT_NEIGHBOURS): a' = a c - b s, b' = b c + a s.  cos_sin: fp32 device array of max_len rows, shared
+ * by the group.  HYDRA_ROT_NONE: rot_dim and cos_sin are not looked at.
+ * q_g [n_tok, ld_q] (table NULL: queries are left alone) receives the query heads, rotated, in bf16; it may be qkv_g with ld_q = ld_qkv.
+ * A page's scale of a head is max(scale before, largest |x| of the new tokens / Q, 2^-126), Q = 127 or 448; a page whose first slot is new
+ * has no scale before.  Where it grows, codes that the page holds become round(code * (before / scale)); new codes are
+ * round(x * (1 / scale)), to nearest even.  Infinities become the largest code and do not count for a scale, NaN becomes 0.  Slots past a
+ * sequence's last token keep what they have.  A page may belong to one sequence of the call only, unless nothing is appended to it.
+ * Tokens at positions below 0 (lens[b] less than the tokens of the call) are dropped. */
+int hydra_op_cache_append(const hydra_cache_desc* cache, int H, int ld_qkv, int ld_q, int rot, int rot_dim, const float* cos_sin,
+                          const void* const* qkv, void* const* q, void* stream);
+
+/* o_i = sum_t softmax_t(scale * q_i . k_t) v_t over the tokens t that the cache holds of the row's sequence, with causal those up to the
+ * row's own position.  q_g [n_tok, ld_q] and o_g [n_tok, ld_o] bf16, H heads of DH columns; query head i reads key/value head i / (H/HKV).
+ * lse_g (table NULL: not wanted) [n_tok, H] fp32: log-sum-exp of the scaled scores.  A row that sees no token gets o = 0 and lse = -inf.
+ * o_g may be q_g with the same leading dimension.  q, o 16-byte aligned, ld_q and ld_o multiples of 8.  What slots past a sequence's
+ * length hold does not matter; codes of its tokens are numbers (hydra_op_cache_append stores no NaN).
+ * ws_g: device scratch of hydra_op_cache_attention_ws_bytes bytes, 16-byte aligned, so that a sequence's tokens can be split over
+ * workgroups whose results are joined in ascending order; it need not be initialised.  Without it (or with too little) nothing is split.
+ * The size and the split depend on the descriptor's sizes and H alone. */
+int hydra_op_cache_attention(const hydra_cache_desc* cache, int H, int ld_q, int ld_o, int causal, float scale, const void* const* q,
+                             void* const* o, float* const* lse, void* const* ws, size_t ws_bytes, void* stream);
+size_t hydra_op_cache_attention_ws_bytes(const hydra_cache_desc* cache, int H);
+
+/* One token per row of logits_g [rows, ldz] (fp32 or bf16, V columns), drawn from given uniforms u_g [rows, ldu] in [0, 1), one per token.
+ * temperature, top_k, top_p, min_p: device arrays of `rows` entries, shared by the group.  With tokens in order of falling logits (the lower index
+ * first among equals) and w_i = exp((z_i - max z) / temperature), kept are the first top_k (0: all); of those the shortest run from the first on
+ * whose sum of w reaches top_p times the sum over all of them (top_p >= 1: all, at least one token always); of those the tokens with w_i >= min_p
+ * times the largest.  token_g[row] = argmax over the kept of z_i / temperature - log(-log u_i), which draws i with probability proportional to
+ * w_i; temperature <= 0: the largest logit.  logprob_g[row] (table NULL: not wanted) = log softmax(z)[token], over all tokens at temperature 1.
+ * Logits of -inf or NaN are never drawn, +inf counts as the largest fp32 number; a row without a token to draw gets -1 and -inf. */
+int hydra_op_sample(int dtype, int rows, int V, int ldz, int ldu, int G, const void* const* logits, const float* const* u,
+                    const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int32_t* const* token,
+                    float* const* logprob, void* stream);
+
 /* Measurement aid: enqueues n launches of a kernel that does nothing (one wave) on `stream`.  The time per launch of
  * a long run of them is the floor under any step that is a chain of dependent launches, which is what bounds the
  * smallest workload (its whole step is microseconds of arithmetic). */

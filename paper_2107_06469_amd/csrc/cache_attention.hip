@@ -1,0 +1,384 @@
+// Attention of new tokens over a paged cache of 8-bit codes (kv_cache.hip writes it).
+//   s[i,t] = (q_i . k_t) * scale,  k_t = code_t * s_page;  t < length, and t <= position of i under a causal mask;  p = softmax over t;
+//   o_i = sum_t p[i,t] v_t,  lse_i = log sum_t exp s[i,t];  a row that sees nothing: o = 0, lse = -inf.
+// The rows of one key/value head are all its query heads of all tokens of the call, (token, head) in that order, so that every code is read once
+// for all of them.
+//
+// Codes never leave registers between memory and the matrix cores.  Both products run on v_mfma_f32_16x16x32_f16: codes are exact in f16 (11
+// bits), p in f16 is rounded to 2^-12, finer than bf16 would, and a query row, bf16, is exact in f16 once the power of two of its largest
+// element is taken out (what is 2^-24 of that or less loses bits).
+//   S^T[t,i] = K Q^T:  lane l supplies row t = l%16 of K, 16 bytes at a time as they lie in memory, and gets column i = l%16, rows 4(l/16) + e
+//   O^T[d,i] += V^T P^T: the accumulators of two 16-key tiles are, in that order, the B operand (k index = accumulator row), and the A operand is,
+//     for d = W (l%16) + c (W = DH/16 bytes, one load), byte c of the 8 keys' words: one byte permutation brings two keys' codes together.
+// A page's scale multiplies scores (keys) or probabilities (values, in units of 2^-15 of the largest scale met so far: f16 then holds weights down
+// to 2^-39 of the largest).
+#include <algorithm>
+
+#include "kernels.h"
+#include "wave_math.h"
+
+namespace hydra {
+namespace {
+
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+constexpr float NEG_BIG = -1.0e30f;
+constexpr float P_ONE = 32768.f;  // a weight of 1 in f16
+
+__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+  const f32x2 v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const f16x2 v = {(_Float16)a, (_Float16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ f32x4 mfma16(const uint4& a, const uint4& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// int8 codes in the low bytes of two halves -> f16: with the sign bit turned over a code c is 128 + c, which under the exponent of 1024 is 1152 + c
+__device__ __forceinline__ uint32_t int8_halves(uint32_t w) {
+  const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, w ^ 0x64806480u) - off);
+}
+template <bool HI>
+__device__ __forceinline__ uint32_t e4m3_halves(uint32_t w) {
+  return __builtin_bit_cast(uint32_t, (f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HI));
+}
+// the low (high) two codes of a word as f16
+template <int KIND, bool HI>
+__device__ __forceinline__ uint32_t halves(uint32_t w) {
+  if (KIND == CACHE_E4M3) return e4m3_halves<HI>(w);
+  return int8_halves(__builtin_amdgcn_perm(0, w, HI ? 0x0c030c02u : 0x0c010c00u));
+}
+// eight codes in a row
+template <int KIND>
+__device__ __forceinline__ uint4 wide8(uint32_t lo, uint32_t hi) {
+  return make_uint4(halves<KIND, false>(lo), halves<KIND, true>(lo), halves<KIND, false>(hi), halves<KIND, true>(hi));
+}
+// bytes C and C + 1 (C even) of two keys' words -> {key 0, key 1} of column C and of column C + 1
+template <int KIND, int C>
+__device__ __forceinline__ uint2 columns2(uint32_t k0, uint32_t k1) {
+  if (KIND == CACHE_E4M3) {
+    const uint32_t w = __builtin_amdgcn_perm(k1, k0, (unsigned)C | (4u + C) << 8 | (1u + C) << 16 | (5u + C) << 24);
+    return make_uint2(e4m3_halves<false>(w), e4m3_halves<true>(w));
+  }
+  return make_uint2(int8_halves(__builtin_amdgcn_perm(k1, k0, 0x0c000c00u | C | (4u + C) << 16)),
+                    int8_halves(__builtin_amdgcn_perm(k1, k0, 0x0c000c00u | (C + 1) | (5u + C) << 16)));
+}
+
+// max over the four lanes that share l%16
+__device__ __forceinline__ float quarter_max(float v) {
+  float2 p = wave_swap32(v);
+  v = fmaxf(p.x, p.y);
+  p = wave_swap16(v);
+  return fmaxf(p.x, p.y);
+}
+__device__ __forceinline__ float quarter_sum(float v) {
+  float2 p = wave_swap32(v);
+  v = p.x + p.y;
+  p = wave_swap16(v);
+  return p.x + p.y;
+}
+
+__device__ __forceinline__ int lane_int(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ float lane_float(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
+
+struct CacheAttnPlan {
+  int n_split, chunk;  // runs of keys, keys in one (a multiple of 128)
+  int n_rt;            // 16-row tiles of the sequence with the most rows
+  int page_log2;
+};
+
+// Four waves share a run of keys, 32 at a time in turn, each with its own maximum, sum and accumulators; they are joined through LDS.
+// blockIdx: x sequence and key/value head, y run of keys and row tile, z model.
+template <int KIND, int DH>
+__global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, const CacheAttnPlan pl) {
+  constexpr int W = DH / 16, NK = DH / 32, NL = DH / 64;  // bytes of a V load; k steps of a score; K loads of 16 bytes per lane
+  __shared__ float2 w_ml[4][16];
+  __shared__ __attribute__((aligned(16))) float w_o[4][16][DH + 4];
+  const CacheArgs& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, gq = lane >> 4;
+  const int g = blockIdx.z, b = blockIdx.x / c.HKV, h = blockIdx.x - b * c.HKV;
+  const int split = blockIdx.y / pl.n_rt, rt = blockIdx.y - split * pl.n_rt;
+  const CacheSeq sq = cache_seq(c, b);
+  const int share = a.H / c.HKV, rows = sq.n * share, first = rt * 16;
+  if (first >= rows) return;
+  // this lane's row
+  const bool have = first + r < rows;
+  const int row = have ? first + r : first, j = row / share, hq = h * share + row - j * share;
+  const int sees = have ? (a.causal ? max(sq.pos0 + j + 1, 0) : sq.len) : 0;  // keys
+  const int all = a.causal ? max(sq.pos0 + (min(first + 16, rows) - 1) / share + 1, 0) : sq.len;
+  const int t_lo = split * pl.chunk, t_hi = min(t_lo + pl.chunk, all);
+
+  uint4 qf[NK];
+  float q_scale;
+  {
+    const bf16_t* q = a.q[g] + (size_t)(sq.row0 + j) * a.ld_q + (size_t)hq * DH;
+    float x[NK][8];
+    float most = 0.f;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+      const uint4 w = *reinterpret_cast<const uint4*>(q + ((k >> 1) * 4 + gq) * 16 + (k & 1) * 8);
+      const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[k][2 * e] = __uint_as_float(v[e] << 16), x[k][2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+        most = fmaxf(most, fmaxf(fabsf(x[k][2 * e]), fabsf(x[k][2 * e + 1])));
+      }
+    }
+    most = quarter_max(most);
+    const unsigned ex = min(max(__float_as_uint(most) >> 23, 1u), 253u);
+    const float f = __uint_as_float((254u - ex) << 23);
+    q_scale = __uint_as_float(ex << 23) * (a.scale * LOG2E);
+#pragma unroll
+    for (int k = 0; k < NK; ++k)
+      qf[k] = make_uint4(pack_f16(x[k][0] * f, x[k][1] * f), pack_f16(x[k][2] * f, x[k][3] * f), pack_f16(x[k][4] * f, x[k][5] * f),
+                         pack_f16(x[k][6] * f, x[k][7] * f));
+  }
+
+  f32x4 acc[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = NEG_BIG, l = 0.f, unit = 0.f;  // unit: what the accumulators are to be multiplied by
+  const int page_mask = c.page - 1;
+  for (int seg = t_lo; seg < t_hi; seg += 64 << pl.page_log2) {
+    const int seg_hi = min(t_hi, seg + (64 << pl.page_log2));
+    // lane i knows the segment's page i
+    int id = -1;
+    float ks = 0.f, vs = 0.f;
+    if (seg + (lane << pl.page_log2) < seg_hi) {
+      id = c.table[(size_t)b * c.max_pages + (seg >> pl.page_log2) + lane];
+      if ((unsigned)id >= (unsigned)c.n_pages) id = -1;
+      else ks = c.ks[g][(size_t)id * c.HKV + h], vs = c.vs[g][(size_t)id * c.HKV + h];
+    }
+    const float unit_now = fmaxf(unit, wave_max(vs));
+    const float again = unit_now > 0.f ? unit / unit_now : 0.f;
+    vs = unit_now > 0.f ? vs / unit_now * P_ONE : 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) acc[i] *= again;
+    unit = unit_now;
+    for (int t = seg + wave * 32; t < seg_hi; t += 128) {
+      uint4 kw[2][NL];
+      uint2 vw[2][4];
+      float kf[2], vf[2];
+      bool ok[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int ts = t + 16 * s, pg = (ts - seg) >> pl.page_log2;
+        const int pid = lane_int(id, pg & 63);
+        ok[s] = pid >= 0 && ts < seg_hi;
+        kf[s] = lane_float(ks, pg & 63) * q_scale, vf[s] = lane_float(vs, pg & 63);
+        const size_t at = (size_t)max(pid, 0) * c.page_bytes + ((size_t)h * c.page + (ts & page_mask)) * DH;
+        const uint8_t* kp = c.k[g] + at + r * DH + gq * 16;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) kw[s][i] = *reinterpret_cast<const uint4*>(kp + 64 * i);
+        const uint8_t* vp = c.v[g] + at + gq * 4 * DH + r * W;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (W == 8) vw[s][e] = *reinterpret_cast<const uint2*>(vp + e * DH);
+          else vw[s][e] = make_uint2(*reinterpret_cast<const uint32_t*>(vp + e * DH), 0u);
+        }
+        if (KIND == CACHE_E4M3 && (!ok[s] || ts + 16 > seg_hi)) {  // what no token has written may be a NaN
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!ok[s] || ts + 4 * gq + e >= seg_hi) vw[s][e] = make_uint2(0u, 0u);
+        }
+      }
+      float p[2][4];
+      float top = m;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+          const uint4& w = kw[s][k >> 1];
+          z = mfma16(k & 1 ? wide8<KIND>(w.z, w.w) : wide8<KIND>(w.x, w.y), qf[k], z);
+        }
+        const int left = ok[s] ? min(sees, seg_hi) - (t + 16 * s) - 4 * gq : 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[s][e] = e < left ? z[e] * kf[s] : -__builtin_inff();
+          top = fmaxf(top, p[s][e]);
+        }
+      }
+      top = quarter_max(top);
+      const float keep = fast_exp2(m - top);
+      m = top;
+      float sum = 0.f;
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[s][e] = fast_exp2(p[s][e] - top);
+          sum += p[s][e];
+        }
+      l = l * keep + sum;
+#pragma unroll
+      for (int i = 0; i < W; ++i) acc[i] *= keep;
+      const uint4 pf = make_uint4(pack_f16(p[0][0] * vf[0], p[0][1] * vf[0]), pack_f16(p[0][2] * vf[0], p[0][3] * vf[0]),
+                                  pack_f16(p[1][0] * vf[1], p[1][1] * vf[1]), pack_f16(p[1][2] * vf[1], p[1][3] * vf[1]));
+      auto value = [&](auto c_) {
+        constexpr int C = decltype(c_)::value, B = C & 3;
+        auto word = [&](int s, int e) { return C < 4 ? vw[s][e].x : vw[s][e].y; };
+        const uint2 a0 = columns2<KIND, B>(word(0, 0), word(0, 1)), a1 = columns2<KIND, B>(word(0, 2), word(0, 3));
+        const uint2 a2 = columns2<KIND, B>(word(1, 0), word(1, 1)), a3 = columns2<KIND, B>(word(1, 2), word(1, 3));
+        acc[C] = mfma16(make_uint4(a0.x, a1.x, a2.x, a3.x), pf, acc[C]);
+        acc[C + 1] = mfma16(make_uint4(a0.y, a1.y, a2.y, a3.y), pf, acc[C + 1]);
+      };
+      value(std::integral_constant<int, 0>{});
+      value(std::integral_constant<int, 2>{});
+      if constexpr (W == 8) {
+        value(std::integral_constant<int, 4>{});
+        value(std::integral_constant<int, 6>{});
+      }
+    }
+  }
+  l = quarter_sum(l);
+
+  if (gq == 0) w_ml[wave][r] = make_float2(m, l);
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+#pragma unroll
+    for (int i = 0; i < W; i += 4) {
+      const f32x4 v = f32x4{acc[i][e], acc[i + 1][e], acc[i + 2][e], acc[i + 3][e]} * (unit * (1.0f / P_ONE));
+      *reinterpret_cast<f32x4*>(&w_o[wave][r][W * (4 * gq + e) + i]) = v;
+    }
+  __syncthreads();
+  const int jr = tid >> 4, d0 = (tid & 15) * W;  // joined by 16 threads a row, W columns each
+  if (first + jr >= rows) return;
+  float mm = NEG_BIG;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) mm = fmaxf(mm, w_ml[w][jr].x);
+  float ll = 0.f, o[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) o[i] = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = fast_exp2(w_ml[w][jr].x - mm);
+    ll += w_ml[w][jr].y * f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) o[i] += w_o[w][jr][d0 + i] * f;
+  }
+  const int tok = sq.row0 + (first + jr) / share, head = h * share + (first + jr) % share;
+  if (pl.n_split == 1) {
+    const float f = ll > 0.f ? 1.0f / ll : 0.f;
+    uint32_t* dst = reinterpret_cast<uint32_t*>(a.o[g] + (size_t)tok * a.ld_o + (size_t)head * DH + d0);
+#pragma unroll
+    for (int i = 0; i < W; i += 2) dst[i >> 1] = pack_bf16(o[i] * f, o[i + 1] * f);
+    if (a.lse[g] && (tid & 15) == 0) a.lse[g][(size_t)tok * a.H + head] = ll > 0.f ? mm * LN2 + __logf(ll) : -__builtin_inff();
+  } else {
+    const size_t part = ((size_t)tok * a.H + head) * pl.n_split + split;
+    float* po = static_cast<float*>(a.ws[g]) + part * DH + d0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) po[i] = o[i];
+    float2* ml = reinterpret_cast<float2*>(static_cast<float*>(a.ws[g]) + (size_t)c.n_tok * a.H * pl.n_split * DH);
+    if ((tid & 15) == 0) ml[part] = make_float2(mm, ll);
+  }
+}
+
+// The runs' partial sums of one row and head, in ascending order: one wave each.
+template <int DH>
+__global__ __launch_bounds__(256) void cache_attn_join_kernel(const CacheAttnArgs a, const CacheAttnPlan pl) {
+  constexpr int E = DH / 64;
+  const int g = blockIdx.y, lane = threadIdx.x & 63;
+  const int64_t n = (int64_t)a.c.n_tok * a.H, i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (i >= n) return;
+  const int tok = (int)(i / a.H), head = (int)(i - (int64_t)tok * a.H);
+  const float* po = static_cast<const float*>(a.ws[g]) + (size_t)i * pl.n_split * DH + lane * E;
+  const float2* ml = reinterpret_cast<const float2*>(static_cast<const float*>(a.ws[g]) + (size_t)n * pl.n_split * DH) + (size_t)i * pl.n_split;
+  float mm = NEG_BIG;
+  for (int s = 0; s < pl.n_split; ++s) mm = fmaxf(mm, ml[s].x);
+  float ll = 0.f, o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  for (int s = 0; s < pl.n_split; ++s) {
+    const float2 v = ml[s];
+    if (v.y > 0.f || v.y != v.y) {
+      const float f = fast_exp2(v.x - mm);
+      ll += v.y * f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] += po[(size_t)s * DH + e] * f;
+    }
+  }
+  const float f = ll > 0.f ? 1.0f / ll : (ll == 0.f ? 0.f : ll);
+  bf16_t* dst = a.o[g] + (size_t)tok * a.ld_o + (size_t)head * DH + lane * E;
+  if (E == 2) *reinterpret_cast<uint32_t*>(dst) = pack_bf16(o[0] * f, o[E - 1] * f);
+  else *dst = (bf16_t)pack_bf16(o[0] * f, 0.f);
+  if (a.lse[g] && lane == 0) a.lse[g][i] = ll > 0.f ? mm * LN2 + __logf(ll) : (ll == 0.f ? -__builtin_inff() : ll);
+}
+
+int floor_log2(int v) { return 31 - __builtin_clz((unsigned)v); }
+
+CacheAttnPlan plan_of(const CacheArgs& c, int H) {
+  CacheAttnPlan p{};
+  p.page_log2 = floor_log2(c.page);
+  p.n_rt = (int)(((int64_t)c.max_q * (H / c.HKV) + 15) / 16);
+  const int64_t base = (int64_t)c.G * c.B * c.HKV * p.n_rt, want = base >= 4096 ? 1 : (1024 + base - 1) / base;
+  const int64_t most = (c.max_len + 127) / 128;
+  int64_t n = std::min(std::max<int64_t>(want, base >= 4096 ? 1 : (c.max_len + 1023) / 1024), most);
+  if (n < 1) n = 1;
+  p.chunk = (int)(((c.max_len + n - 1) / n + 127) / 128 * 128);
+  p.n_split = (c.max_len + p.chunk - 1) / p.chunk;
+  return p;
+}
+
+}  // namespace
+
+size_t cache_attn_ws_bytes(const CacheArgs& c, int H) {
+  const CacheAttnPlan p = plan_of(c, H);
+  return p.n_split == 1 ? 0 : (size_t)c.n_tok * H * p.n_split * (c.DH + 2) * sizeof(float);
+}
+
+const char* cache_attn_sizes_refusal(const CacheArgs& c, int H) {
+  if (const char* why = cache_sizes_refusal(c)) return why;
+  if (H < 1 || H % c.HKV) return "H is no multiple of HKV";
+  if ((int64_t)c.max_q * (H / c.HKV) > 0x7fffffffLL - 1024) return "too many rows of one key/value head";
+  return nullptr;
+}
+
+const char* cache_attn_refusal(const CacheAttnArgs& a) {
+  if (const char* why = cache_refusal(a.c)) return why;
+  const CacheArgs& c = a.c;
+  if (const char* why = cache_attn_sizes_refusal(c, a.H)) return why;
+  if (a.ld_q % 8 || a.ld_o % 8 || (int64_t)a.ld_q < (int64_t)a.H * c.DH || (int64_t)a.ld_o < (int64_t)a.H * c.DH)
+    return "ld_q or ld_o is less than a row or no multiple of 8";
+  if (!(a.scale > 0.f) || a.scale > 1e30f) return "scale is positive and finite";
+  for (int g = 0; g < c.G; ++g) {
+    if (!a.q[g] || !a.o[g] || ((uintptr_t)a.q[g] | (uintptr_t)a.o[g]) % 16) return "q or o is NULL or not 16-byte aligned";
+    if ((a.lse[g] != nullptr) != (a.lse[0] != nullptr)) return "lse for all models or for none";
+    if ((a.ws[g] != nullptr) != (a.ws[0] != nullptr) || (uintptr_t)a.ws[g] % 16) return "ws for all models or for none, 16-byte aligned";
+  }
+  return nullptr;
+}
+
+hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t s) {
+  const CacheArgs& c = a.c;
+  CacheAttnPlan p = plan_of(c, a.H);
+  if (p.n_split > 1 && (!a.ws[0] || a.ws_bytes < cache_attn_ws_bytes(c, a.H))) p.n_split = 1, p.chunk = (c.max_len + 127) / 128 * 128;
+  const int64_t bh = (int64_t)c.B * c.HKV, sr = (int64_t)p.n_split * p.n_rt;
+  if (bh > 0x7fffffffLL || sr > 65535) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)bh, (unsigned)sr, c.G);
+  if (c.kind == CACHE_INT8) {
+    if (c.DH == 64) hipLaunchKernelGGL((cache_attn_kernel<CACHE_INT8, 64>), grid, dim3(256), 0, s, a, p);
+    else hipLaunchKernelGGL((cache_attn_kernel<CACHE_INT8, 128>), grid, dim3(256), 0, s, a, p);
+  } else {
+    if (c.DH == 64) hipLaunchKernelGGL((cache_attn_kernel<CACHE_E4M3, 64>), grid, dim3(256), 0, s, a, p);
+    else hipLaunchKernelGGL((cache_attn_kernel<CACHE_E4M3, 128>), grid, dim3(256), 0, s, a, p);
+  }
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (p.n_split == 1) return hipSuccess;
+  const dim3 join((unsigned)(((int64_t)c.n_tok * a.H + 3) / 4), c.G);
+  if (c.DH == 64) hipLaunchKernelGGL((cache_attn_join_kernel<64>), join, dim3(256), 0, s, a, p);
+  else hipLaunchKernelGGL((cache_attn_join_kernel<128>), join, dim3(256), 0, s, a, p);
+  return hipGetLastError();
+}
+
+}  // namespace hydra

@@ -280,6 +280,74 @@ struct AttnBwdArgs {
 hipError_t launch_attn_bwd(const AttnBwdArgs& a, hipStream_t s);
 hipError_t attn_init();
 
+// ---- a paged cache of keys and values in 8 bits (kv_cache.hip, cache_attention.hip) ------------------------------
+// Page p of a pool: [HKV, page, DH] codes, page_bytes from page to page; its scale of head h at [p*HKV + h].  Sequence b's tokens
+// [i*page, (i+1)*page) lie in page table[b*max_pages + i]; a page id out of range holds nothing.
+enum { CACHE_INT8 = 0, CACHE_E4M3 = 1 };
+enum { ROT_NONE = 0, ROT_HALVES = 1, ROT_NEIGHBOURS = 2 };
+struct CacheArgs {
+  int kind, B, HKV, DH, page, n_pages, max_pages, G;
+  int n_tok, max_q, max_len;  // rows of the call; the most of one sequence; the longest sequence
+  size_t page_bytes;
+  const int32_t* table;  // [B, max_pages]
+  const int32_t* lens;   // [B] tokens in the cache, the call's included
+  const int32_t* q_ptr;  // [B+1] rows of a sequence's tokens, or null: row b
+  uint8_t* k[MAXG];
+  uint8_t* v[MAXG];
+  float* ks[MAXG];
+  float* vs[MAXG];
+};
+struct CacheSeq { int row0, n, len, pos0; };  // the call's first row and rows of a sequence, its length, the first row's position
+// What the device arrays say of sequence b, held to the bounds that the host has given.
+__device__ __forceinline__ CacheSeq cache_seq(const CacheArgs& c, int b) {
+  CacheSeq s;
+  s.len = min(max(c.lens[b], 0), c.max_len);
+  s.row0 = c.q_ptr ? min(max(c.q_ptr[b], 0), c.n_tok) : b;
+  s.n = c.q_ptr ? min(max(min(c.q_ptr[b + 1], c.n_tok) - s.row0, 0), c.max_q) : 1;
+  s.pos0 = s.len - s.n;
+  return s;
+}
+struct AppendArgs {
+  CacheArgs c;
+  int H, ld_qkv, ld_q, rot, rot_dim, has_q;
+  int cache_blocks;        // set by the launcher
+  const float* cs;         // [max_len, rot_dim] cosines, then sines
+  const bf16_t* qkv[MAXG];
+  bf16_t* q[MAXG];
+};
+const char* cache_refusal(const CacheArgs& c);  // null, or what is wrong
+const char* append_refusal(const AppendArgs& a);
+hipError_t launch_append(const AppendArgs& a, hipStream_t s);
+struct CacheAttnArgs {
+  CacheArgs c;
+  int H, ld_q, ld_o, causal;
+  float scale;
+  const bf16_t* q[MAXG];
+  bf16_t* o[MAXG];
+  float* lse[MAXG];  // [n_tok, H], all or none
+  void* ws[MAXG];    // scratch of cache_attn_ws_bytes, all or none: without it nothing is split
+  size_t ws_bytes;
+};
+const char* cache_sizes_refusal(const CacheArgs& c);  // the part that needs no pointers
+const char* cache_attn_sizes_refusal(const CacheArgs& c, int H);
+const char* cache_attn_refusal(const CacheAttnArgs& a);
+size_t cache_attn_ws_bytes(const CacheArgs& c, int H);
+hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t s);
+
+// ---- drawing tokens (sample.hip) -----------------------------------------------------------------------------------
+struct SampleArgs {
+  int dtype, rows, V, ldz, ldu, G;
+  const float* temperature;  // [rows], shared by the group, like top_k, top_p and min_p
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const void* z[MAXG];
+  const float* u[MAXG];
+  int32_t* token[MAXG];
+  float* logprob[MAXG];  // all or none
+};
+hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
+
 // all per-process kernel set-up (LDS limits); call once before the first launch
 hipError_t kernels_init();
 

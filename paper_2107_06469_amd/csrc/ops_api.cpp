@@ -252,3 +252,77 @@ int hydra_op_cast_bf16(const float* src, void* dst, size_t n, void* stream) {
 }
 
 }  // extern "C"
+
+static CacheArgs cache_args(const hydra_cache_desc* d) {
+  CacheArgs c{};
+  c.kind = d->kind; c.B = d->B; c.HKV = d->HKV; c.DH = d->DH; c.page = d->page; c.n_pages = d->n_pages; c.max_pages = d->max_pages; c.G = d->G;
+  c.n_tok = d->n_tok; c.max_q = d->max_q; c.max_len = d->max_len;
+  c.page_bytes = d->page_bytes ? d->page_bytes : (size_t)(d->HKV > 0 ? d->HKV : 0) * (d->page > 0 ? d->page : 0) * (d->DH > 0 ? d->DH : 0);
+  c.table = d->page_table; c.lens = d->lens; c.q_ptr = d->q_ptr;
+  for (int g = 0; g < d->G; ++g) {
+    c.k[g] = static_cast<uint8_t*>(d->k[g]); c.v[g] = static_cast<uint8_t*>(d->v[g]);
+    c.ks[g] = d->k_scale[g]; c.vs[g] = d->v_scale[g];
+  }
+  return c;
+}
+static bool cache_tables(const hydra_cache_desc* d) {
+  return d && d->k && d->v && d->k_scale && d->v_scale && d->G >= 1 && d->G <= MAXG;
+}
+
+extern "C" {
+
+int hydra_op_cache_append(const hydra_cache_desc* d, int H, int ld_qkv, int ld_q, int rot, int rot_dim, const float* cos_sin,
+                          const void* const* qkv, void* const* q, void* stream) {
+  if (!cache_tables(d) || !qkv) return bad("hydra_op_cache_append: NULL table or G out of range");
+  AppendArgs a{};
+  a.c = cache_args(d);
+  a.H = H; a.ld_qkv = ld_qkv; a.ld_q = ld_q; a.rot = rot; a.rot_dim = rot_dim; a.cs = cos_sin; a.has_q = q != nullptr;
+  for (int g = 0; g < d->G; ++g) {
+    a.qkv[g] = static_cast<const bf16_t*>(qkv[g]);
+    a.q[g] = q ? static_cast<bf16_t*>(q[g]) : nullptr;
+  }
+  if (const char* why = append_refusal(a)) return ops_fail(HYDRA_ERR_INVALID_ARG, "hydra_op_cache_append", why);
+  return done(launch_append(a, static_cast<hipStream_t>(stream)), "hydra_op_cache_append");
+}
+
+size_t hydra_op_cache_attention_ws_bytes(const hydra_cache_desc* d, int H) {
+  if (!cache_tables(d)) return 0;
+  const CacheArgs c = cache_args(d);
+  return cache_attn_sizes_refusal(c, H) ? 0 : cache_attn_ws_bytes(c, H);
+}
+
+int hydra_op_cache_attention(const hydra_cache_desc* d, int H, int ld_q, int ld_o, int causal, float scale, const void* const* q,
+                             void* const* o, float* const* lse, void* const* ws, size_t ws_bytes, void* stream) {
+  if (!cache_tables(d) || !q || !o) return bad("hydra_op_cache_attention: NULL table or G out of range");
+  CacheAttnArgs a{};
+  a.c = cache_args(d);
+  a.H = H; a.ld_q = ld_q; a.ld_o = ld_o; a.causal = causal; a.scale = scale; a.ws_bytes = ws ? ws_bytes : 0;
+  for (int g = 0; g < d->G; ++g) {
+    a.q[g] = static_cast<const bf16_t*>(q[g]);
+    a.o[g] = static_cast<bf16_t*>(o[g]);
+    a.lse[g] = lse ? lse[g] : nullptr;
+    a.ws[g] = ws ? ws[g] : nullptr;
+  }
+  if (const char* why = cache_attn_refusal(a)) return ops_fail(HYDRA_ERR_INVALID_ARG, "hydra_op_cache_attention", why);
+  return done(launch_cache_attn(a, static_cast<hipStream_t>(stream)), "hydra_op_cache_attention");
+}
+
+int hydra_op_sample(int dtype, int rows, int V, int ldz, int ldu, int G, const void* const* logits, const float* const* u,
+                    const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int32_t* const* token,
+                    float* const* logprob, void* stream) {
+  if (!logits || !u || !temperature || !top_k || !top_p || !min_p || !token || G < 1 || G > MAXG)
+    return bad("hydra_op_sample: NULL table or G out of range");
+  if (dtype != HYDRA_OPS_F32 && dtype != HYDRA_OPS_BF16) return bad("hydra_op_sample: unknown dtype");
+  SampleArgs a{};
+  a.dtype = dtype == HYDRA_OPS_F32 ? GEMM_F32 : GEMM_BF16;
+  a.rows = rows; a.V = V; a.ldz = ldz; a.ldu = ldu; a.G = G;
+  a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p;
+  for (int g = 0; g < G; ++g) {
+    if (!logits[g] || !u[g] || !token[g] || (logprob && !logprob[g])) return bad("hydra_op_sample: NULL entry");
+    a.z[g] = logits[g]; a.u[g] = u[g]; a.token[g] = token[g];
+    a.logprob[g] = logprob ? logprob[g] : nullptr;
+  }
+  return done(launch_sample(a, static_cast<hipStream_t>(stream)), "hydra_op_sample");
+}
+
+}  // extern "C"

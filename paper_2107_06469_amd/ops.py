@@ -12,6 +12,8 @@ from array import array
 from .hydra import HydraError, lib
 
 F32, BF16 = 0, 1
+CACHE_INT8, CACHE_E4M3 = 0, 1
+ROT_NONE, ROT_HALVES, ROT_NEIGHBOURS = 0, 1, 2
 EPI_NONE, EPI_RELU, EPI_GELU = 0, 1, 2
 
 
@@ -58,6 +60,11 @@ def _L():
         L.hydra_op_attention_bwd.argtypes = [C.c_int] * 7 + [C.c_float, C.c_int] + [pp] * 6 + [vp]
         L.hydra_op_embed_fwd.argtypes = [C.c_int] * 6 + [vp, pp, pp, pp, vp]
         L.hydra_op_embed_bwd.argtypes = [C.c_int] * 8 + [vp, vp, pp, pp, pp, vp]
+        L.hydra_op_cache_append.argtypes = [vp] + [C.c_int] * 5 + [vp, pp, pp, vp]
+        L.hydra_op_cache_attention.argtypes = [vp] + [C.c_int] * 4 + [C.c_float] + [pp] * 4 + [C.c_size_t, vp]
+        L.hydra_op_cache_attention_ws_bytes.argtypes = [vp, C.c_int]
+        L.hydra_op_cache_attention_ws_bytes.restype = C.c_size_t
+        L.hydra_op_sample.argtypes = [C.c_int] * 6 + [pp, pp, vp, vp, vp, vp, pp, pp, vp]
         L.hydra_op_empty_launches.argtypes = [C.c_int, vp]
         L.hydra_ops_last_error.restype = C.c_char_p
         _ready = True
@@ -208,3 +215,63 @@ def hydra_op_embed_fwd(dtype, tokens, S, d, ld, ids, tok, pos, x):
 def hydra_op_embed_bwd(dtype, V, S, S_table, B, d, ld, row_ptr, positions, dx, dtok, dpos):
     keep, *at = _tabs(dx, dtok, dpos)
     _check(_L().hydra_op_embed_bwd(dtype, V, S, S_table, B, d, ld, len(dx), row_ptr.data_ptr(), positions.data_ptr(), *at, _stream()))
+
+
+class Cache:
+    """One layer's paged cache of G models: pools of 8-bit codes k, v [n_pages, HKV, page, DH] (lists of G tensors), their scales k_scale, v_scale
+    [n_pages, HKV] fp32 and the page table [B, max_pages] int32 that the group shares.  A record of tensors and their addresses: what the
+    cache holds is in the tensors alone.  Pools may be slices along their first dimension's stride (several layers in one tensor)."""
+
+    def __init__(self, kind, k, v, k_scale, v_scale, page_table):
+        self.kind, self.k, self.v, self.k_scale, self.v_scale, self.page_table = kind, k, v, k_scale, v_scale, page_table
+        n_pages, hkv, page, dh = k[0].shape
+        stride = k[0].stride(0)
+        for t in (*k, *v):
+            if t.shape != k[0].shape or t.element_size() != 1 or t.stride() != (stride, page * dh, dh, 1):
+                raise ValueError("pools have one shape [n_pages, HKV, page, DH], one page stride and 1-byte codes, contiguous inside a page")
+        for t in (*k_scale, *v_scale):
+            if tuple(t.shape) != (n_pages, hkv) or t.element_size() != 4 or not t.is_contiguous():
+                raise ValueError("scales are contiguous fp32 [n_pages, HKV]")
+        if not len(k) == len(v) == len(k_scale) == len(v_scale):
+            raise ValueError("k, v, k_scale and v_scale have one tensor per model")
+        if page_table.dim() != 2 or page_table.element_size() != 4 or not page_table.is_contiguous():
+            raise ValueError("page_table is contiguous int32 [B, max_pages]")
+        self.B, self.max_pages = page_table.shape
+        self.HKV, self.page, self.DH, self.G = hkv, page, dh, len(k)
+        self._head = (kind, self.B, hkv, dh, page, n_pages, self.max_pages, self.G)
+        self._stride = stride if n_pages > 1 else 0
+        self._keep, *self._at = _tabs(k, v, k_scale, v_scale)
+
+    def desc(self, lens=None, q_ptr=None, n_tok=None, max_q=1, max_len=None):
+        """The packed hydra_cache_desc of a call."""
+        return _cache_desc(*self._head, self.B if n_tok is None else n_tok, max_q, self.max_pages * self.page if max_len is None else max_len,
+                           self._stride, self.page_table.data_ptr(), 0 if lens is None else lens.data_ptr(),
+                           0 if q_ptr is None else q_ptr.data_ptr(), *self._at)
+
+
+_cache_desc = struct.Struct("11iN7P").pack      # the fields of hydra_cache_desc
+
+
+def hydra_op_cache_append(cache, lens, H, ld_qkv, ld_q, qkv, q=None, *, rot=ROT_NONE, rot_dim=0, cos_sin=None, q_ptr=None, n_tok=None, max_q=1,
+                          max_len=None):
+    """q=None leaves the queries alone; max_len=None: as many tokens as the page table has room for."""
+    keep, *at = _tabs(qkv, q)
+    _check(_L().hydra_op_cache_append(cache.desc(lens, q_ptr, n_tok, max_q, max_len), H, ld_qkv, ld_q, rot, rot_dim,
+                                      None if cos_sin is None else cos_sin.data_ptr(), *at, _stream()))
+
+
+def hydra_op_cache_attention_ws_bytes(cache, H, *, n_tok=None, max_q=1, max_len=None) -> int:
+    return int(_L().hydra_op_cache_attention_ws_bytes(cache.desc(n_tok=n_tok, max_q=max_q, max_len=max_len), H))
+
+
+def hydra_op_cache_attention(cache, lens, H, ld_q, ld_o, causal, scale, q, o, lse=None, *, ws=None, q_ptr=None, n_tok=None, max_q=1, max_len=None):
+    """ws: optional per-model scratch tensors (uint8, hydra_op_cache_attention_ws_bytes bytes) that allow splitting a sequence's tokens."""
+    keep, *at = _tabs(q, o, lse, ws)
+    _check(_L().hydra_op_cache_attention(cache.desc(lens, q_ptr, n_tok, max_q, max_len), H, ld_q, ld_o, int(causal), scale, *at, _nbytes(ws),
+                                         _stream()))
+
+
+def hydra_op_sample(dtype, rows, V, ldz, ldu, logits, u, temperature, top_k, top_p, min_p, token, logprob=None):
+    keep, tz, tu, tt, tl = _tabs(logits, u, token, logprob)
+    _check(_L().hydra_op_sample(dtype, rows, V, ldz, ldu, len(logits), tz, tu, temperature.data_ptr(), top_k.data_ptr(), top_p.data_ptr(),
+                                min_p.data_ptr(), tt, tl, _stream()))

@@ -1,0 +1,90 @@
+"""What the serving operators refuse, before anything is launched (no GPU): the status, the text and that the size query agrees."""
+import ctypes as C
+
+import pytest
+
+from paper_2107_06469_amd import ops
+from paper_2107_06469_amd.hydra import lib
+
+A = 1 << 20                       # an address that is never looked at, well aligned
+
+
+def cache(G=1, table=True, **kw):
+    d = dict(kind=0, B=3, HKV=2, DH=128, page=64, n_pages=10, max_pages=4, G=G, n_tok=3, max_q=1, max_len=256, page_bytes=0, page_table=A, lens=A, q_ptr=0)
+    d.update(kw)
+    tabs = [(C.c_void_p * 16)(*[d.pop(n, A)] * 16) for n in ("k", "v", "k_scale", "v_scale")]
+    packed = ops._cache_desc(*d.values(), *[C.addressof(t) if table else 0 for t in tabs])
+    return packed, tabs
+
+
+def pointers(at=A):
+    return (C.c_void_p * 16)(*[at] * 16)
+
+
+def append(H=4, ld_qkv=1024, ld_q=512, rot=0, rot_dim=0, cs=A, qkv=A, q=A, **kw):
+    d, keep = cache(**kw)
+    st = ops._L().hydra_op_cache_append(d, H, ld_qkv, ld_q, rot, rot_dim, cs, pointers(qkv), pointers(q) if q is not None else None, None)
+    return st, lib().hydra_ops_last_error().decode()
+
+
+def attend(H=4, ld_q=512, ld_o=512, scale=0.1, q=A, o=A, lse=A, ws=None, **kw):
+    d, keep = cache(**kw)
+    st = ops._L().hydra_op_cache_attention(d, H, ld_q, ld_o, 1, scale, pointers(q), pointers(o), pointers(lse), pointers(ws) if ws else None, 0, None)
+    return st, lib().hydra_ops_last_error().decode()
+
+
+CACHE = [dict(kind=2), dict(kind=-1), dict(DH=96), dict(DH=0), dict(page=8), dict(page=48), dict(page=256), dict(B=0), dict(B=70000), dict(HKV=0),
+         dict(n_pages=0), dict(max_pages=0), dict(max_len=0), dict(max_len=257), dict(n_tok=0), dict(max_q=0), dict(max_q=2), dict(n_tok=4),
+         dict(page_bytes=64 * 256 - 16), dict(page_bytes=64 * 256 + 8), dict(page_table=0), dict(lens=0), dict(k=0), dict(v=0), dict(k_scale=0),
+         dict(v_scale=0), dict(k=A + 8), dict(v=A + 1), dict(G=0), dict(G=17), dict(table=False), dict(H=0), dict(H=3), dict(H=-2),
+         dict(max_q=5, n_tok=4, q_ptr=A)]
+
+
+@pytest.mark.parametrize("bad", CACHE + [dict(ld_qkv=1016), dict(ld_qkv=1028), dict(ld_q=504), dict(ld_q=516), dict(qkv=0), dict(qkv=A + 2), dict(q=0),
+                                         dict(q=A + 8), dict(rot=3, rot_dim=64), dict(rot=1, rot_dim=0), dict(rot=1, rot_dim=136),
+                                         dict(rot=2, rot_dim=24), dict(rot=1, rot_dim=64, cs=None)], ids=str)
+def test_append_refuses(bad):
+    st, why = append(**bad)
+    assert st == 1 and why.startswith("hydra_op_cache_append: "), (st, why)
+
+
+@pytest.mark.parametrize("bad", CACHE + [dict(ld_q=504), dict(ld_o=508), dict(ld_o=256), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
+                                         dict(scale=float("inf")), dict(q=0), dict(o=0), dict(q=A + 2), dict(o=A + 4), dict(ws=A + 4)], ids=str)
+def test_attention_refuses(bad):
+    st, why = attend(**bad)
+    assert st == 1 and why.startswith("hydra_op_cache_attention: "), (st, why)
+
+
+def test_attention_scratch_sizes():
+    """0 for what is refused and for short sequences; the same for any number of calls; growing with the sequences."""
+    size = lambda H=4, **kw: ops._L().hydra_op_cache_attention_ws_bytes(cache(**kw)[0], H)  # noqa: E731
+    assert size(kind=5) == 0 and size(H=3) == 0 and size(max_len=100) == 0
+    long = dict(max_pages=1000, max_len=64000)
+    assert size(**long) == size(**long) > 0
+    assert size(**long) % 4 == 0
+
+
+@pytest.mark.parametrize("bad", [dict(dtype=2), dict(rows=0), dict(V=0), dict(V=(1 << 24) + 1, ldz=1 << 25, ldu=1 << 25), dict(ldz=99), dict(ldu=99), dict(G=0), dict(G=17),
+                                 dict(logits=0), dict(u=0), dict(token=0), dict(logprob=0), dict(t=None), dict(k=None), dict(p=None), dict(m=None)], ids=str)
+def test_sample_refuses(bad):
+    a = dict(dtype=0, rows=4, V=100, ldz=100, ldu=100, G=1, logits=A, u=A, t=A, k=A, p=A, m=A, token=A, logprob=A)
+    a.update(bad)
+    st = ops._L().hydra_op_sample(a["dtype"], a["rows"], a["V"], a["ldz"], a["ldu"], a["G"], pointers(a["logits"]), pointers(a["u"]), a["t"], a["k"], a["p"],
+                                  a["m"], pointers(a["token"]), pointers(a["logprob"]), None)
+    assert st == 1 and lib().hydra_ops_last_error().decode().startswith("hydra_op_sample: ")
+
+
+def test_cache_record_checks_its_tensors():
+    import torch
+    k = [torch.zeros((5, 2, 16, 64), dtype=torch.int8)]
+    s, t = [torch.zeros((5, 2))], torch.zeros((3, 2), dtype=torch.int32)
+    ops.Cache(0, k, k, s, s, t)
+    wide = torch.zeros((5, 3, 2, 16, 64), dtype=torch.int8)                            # three layers in one tensor
+    c = ops.Cache(0, [wide[:, 1]], [wide[:, 1]], s, s, t)
+    assert c._stride == 3 * 2 * 16 * 64
+    for bad in (dict(k=[k[0].float()]), dict(k=[k[0].transpose(2, 3)]), dict(v=[k[0][:4]]), dict(k_scale=[s[0].half()]), dict(v_scale=[s[0].t()]),
+                dict(page_table=t.long()), dict(page_table=t[0]), dict(k=k + k)):
+        a = dict(k=k, v=k, k_scale=s, v_scale=s, page_table=t)
+        a.update(bad)
+        with pytest.raises(ValueError):
+            ops.Cache(0, **a)
