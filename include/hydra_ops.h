@@ -199,7 +199,7 @@ int hydra_op_cache_attention(const hydra_cache_desc* cache, int H, int ld_q, int
                              void* const* o, float* const* lse, void* const* ws, size_t ws_bytes, void* stream);
 size_t hydra_op_cache_attention_ws_bytes(const hydra_cache_desc* cache, int H);
 
-/* One token per row of logits_g [rows, ldz] (fp32 or bf16, V columns), drawn from given uniforms u_g [rows, ldu] in [0, 1), one per token.
+/* One token per row of logits_g [rows, ldz] (fp32 or bf16, V columns, 262144 at most), drawn from given uniforms u_g [rows, ldu] in [0, 1), one per token.
  * temperature, top_k, top_p, min_p: device arrays of `rows` entries, shared by the group.  With tokens in order of falling logits (the lower index
  * first among equals) and w_i = exp((z_i - max z) / temperature), kept are the first top_k (0: all); of those the shortest run from the first on
  * whose sum of w reaches top_p times the sum over all of them (top_p >= 1: all, at least one token always); of those the tokens with w_i >= min_p

@@ -346,6 +346,8 @@ struct SampleArgs {
   int32_t* token[MAXG];
   float* logprob[MAXG];  // all or none
 };
+const char* sample_refusal(const SampleArgs& a);  // null, or what is wrong with the sizes
+hipError_t sample_init();
 hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
 
 // all per-process kernel set-up (LDS limits); call once before the first launch

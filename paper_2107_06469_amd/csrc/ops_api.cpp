@@ -322,6 +322,8 @@ int hydra_op_sample(int dtype, int rows, int V, int ldz, int ldu, int G, const v
     a.z[g] = logits[g]; a.u[g] = u[g]; a.token[g] = token[g];
     a.logprob[g] = logprob ? logprob[g] : nullptr;
   }
+  if (const char* why = sample_refusal(a)) return ops_fail(HYDRA_ERR_INVALID_ARG, "hydra_op_sample", why);
+  if (int st = ensure_init()) return st;
   return done(launch_sample(a, static_cast<hipStream_t>(stream)), "hydra_op_sample");
 }
 
