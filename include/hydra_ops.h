@@ -176,8 +176,8 @@ typedef struct {
 /* The call's keys and values into the cache.  qkv_g [n_tok, ld_qkv] bf16: H query heads of DH columns, then HKV key heads, then HKV value heads;
  * 16-byte aligned, ld_qkv a multiple of 8.  The position rotation turns the first rot_dim columns (a multiple of 16) of every query and key head:
  * with c, s = cos_sin[position*rot_dim + i], cos_sin[position*rot_dim + rot_dim/2 + i] and a, b = columns i and i + rot_dim/2
- * (HYDRA_ROT_HALVES) or 2i and 2i + 1 (HYDRA_ROT_NEIGHBOURS): a' = a c - b s, b' = b c + a s.  cos_sin: fp32 device array of max_len rows, shared
- * by the group.  HYDRA_ROT_NONE: rot_dim and cos_sin are not looked at.
+ * (HYDRA_ROT_HALVES) or 2i and 2i + 1 (HYDRA_ROT_NEIGHBOURS): a' = a c - b s, b' = b c + a s.  cos_sin: fp32 device array of max_len rows, 16-byte
+ * aligned, shared by the group.  HYDRA_ROT_NONE: rot_dim and cos_sin are not looked at.
  * q_g [n_tok, ld_q] (table NULL: queries are left alone) receives the query heads, rotated, in bf16; it may be qkv_g with ld_q = ld_qkv.
  * A page's scale of a head is max(scale before, largest |x| of the new tokens / Q, 2^-126), Q = 127 or 448; a page whose first slot is new
  * has no scale before.  Where it grows, codes that the page holds become round(code * (before / scale)); new codes are

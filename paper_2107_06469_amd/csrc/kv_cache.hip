@@ -28,9 +28,10 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 
 // four codes in one word: x * f to nearest even, at most the largest code; NaN becomes 0
 template <int KIND>
-__device__ __forceinline__ uint32_t to_codes(const float* x, float f) {
+__device__ __forceinline__ uint32_t to_codes(float x0, float x1, float x2, float x3, float f) {
 #pragma clang fp contract(off)
   constexpr float TOP = KIND == CACHE_INT8 ? 127.f : 448.f;
+  const float x[4] = {x0, x1, x2, x3};
   float y[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -46,62 +47,62 @@ __device__ __forceinline__ uint32_t to_codes(const float* x, float f) {
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
 }
+// four codes by another scale
 template <int KIND>
-__device__ __forceinline__ void from_codes(uint32_t w, float* x) {
-  if (KIND == CACHE_INT8) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = (float)((int)(w << (24 - 8 * i)) >> 24);
-  } else {
-    typedef __attribute__((ext_vector_type(2))) float f32x2;
-    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
-  }
+__device__ __forceinline__ uint32_t again(uint32_t w, float f) {
+  if (KIND == CACHE_INT8)
+    return to_codes<KIND>((float)((int)(w << 24) >> 24), (float)((int)(w << 16) >> 24), (float)((int)(w << 8) >> 24), (float)((int)w >> 24), f);
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  return to_codes<KIND>(a.x, a.y, b.x, b.y, f);
 }
 
-__device__ __forceinline__ void unpack8(const uint4& w, float* x) {
-  x[0] = bf_lo(w.x), x[1] = bf_hi(w.x), x[2] = bf_lo(w.y), x[3] = bf_hi(w.y);
-  x[4] = bf_lo(w.z), x[5] = bf_hi(w.z), x[6] = bf_lo(w.w), x[7] = bf_hi(w.w);
-}
+// Sixteen values of a row in registers: two runs of 8 columns.
+struct Unit {
+  float x[16];
+  __device__ __forceinline__ void load(const bf16_t* row, int2 at) {
+    const uint4 a = *reinterpret_cast<const uint4*>(row + at.x), b = *reinterpret_cast<const uint4*>(row + at.y);
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[2 * i] = bf_lo(w[i]), x[2 * i + 1] = bf_hi(w[i]);
+  }
+};
 
 // Unit u of a head's row: the two runs of 8 columns that a rotation by halves turns into one another (columns past rot_dim go by in order).
 __device__ __forceinline__ int2 unit_columns(int u, int rot_dim) {
   const int turned = rot_dim >> 4;
   return u < turned ? make_int2(8 * u, 8 * u + (rot_dim >> 1)) : make_int2(16 * u, 16 * u + 8);
 }
-// x: a unit's 16 values (columns at.x + 0..7 and at.y + 0..7); cs: the position's row of the table
-__device__ __forceinline__ void rotate(float* x, int2 at, int rot, int rot_dim, const float* cs) {
+// cs: the position's row of the table.  Of the two kinds of pairs one is this launch's; columns past rot_dim have none.
+template <int ROT>
+__device__ __forceinline__ void rotate(Unit& u, int2 at, int rot_dim, const float* cs) {
 #pragma clang fp contract(off)
-  if (at.y >= rot_dim && at.x >= rot_dim) return;
-  if (rot == ROT_HALVES) {
+  if (ROT == ROT_NONE || at.x >= rot_dim) return;
+  const float* sn = cs + (rot_dim >> 1);
+  float c[8], s[8];
+  const int ca = ROT == ROT_HALVES ? at.x : at.x >> 1, cb = ROT == ROT_HALVES ? at.x + 4 : at.y >> 1;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float c = cs[at.x + i], s = cs[(rot_dim >> 1) + at.x + i], a = x[i], b = x[8 + i];
-      const float ac = a * c, bs = b * s, bc = b * c, as = a * s;
-      x[i] = ac - bs;
-      x[8 + i] = bc + as;
-    }
-  } else {
+  for (int h = 0; h < 2; ++h) {
+    const float4 cv = *reinterpret_cast<const float4*>(cs + (h ? cb : ca)), sv = *reinterpret_cast<const float4*>(sn + (h ? cb : ca));
+    c[4 * h] = cv.x, c[4 * h + 1] = cv.y, c[4 * h + 2] = cv.z, c[4 * h + 3] = cv.w;
+    s[4 * h] = sv.x, s[4 * h + 1] = sv.y, s[4 * h + 2] = sv.z, s[4 * h + 3] = sv.w;
+  }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int first = h ? at.y : at.x;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float c = cs[(first >> 1) + i], s = cs[(rot_dim >> 1) + (first >> 1) + i], a = x[8 * h + 2 * i], b = x[8 * h + 2 * i + 1];
-        const float ac = a * c, bs = b * s, bc = b * c, as = a * s;
-        x[8 * h + 2 * i] = ac - bs;
-        x[8 * h + 2 * i + 1] = bc + as;
-      }
-    }
+  for (int i = 0; i < 8; ++i) {
+    float &a = u.x[ROT == ROT_HALVES ? i : 2 * i], &b = u.x[ROT == ROT_HALVES ? 8 + i : 2 * i + 1];
+    const float ac = a * c[i], bs = b * s[i], bc = b * c[i], as = a * s[i];
+    a = ac - bs;
+    b = bc + as;
   }
 }
 
 // NT threads; a page's new rows are at most NT * UPT units.  blockIdx: x the pages and heads of keys and values, then the runs of query rows;
 // y the sequence; z the model.
-template <int KIND, int NT, int UPT>
+template <int KIND, int ROT, int NT, int UPT>
 __global__ __launch_bounds__(NT) void append_kernel(const AppendArgs a) {
   const CacheArgs& c = a.c;
   const int g = blockIdx.z, b = blockIdx.y, tid = threadIdx.x;
-  const int upr = c.DH >> 4;  // units per head's row
+  const int upr_log2 = c.DH == 128 ? 3 : 2, upr = 1 << upr_log2;  // units per head's row
   const CacheSeq s = cache_seq(c, b);
   const bf16_t* const qkv = a.qkv[g] + (size_t)s.row0 * a.ld_qkv;
   int x = blockIdx.x;
@@ -109,16 +110,14 @@ __global__ __launch_bounds__(NT) void append_kernel(const AppendArgs a) {
     x -= a.cache_blocks;
     const int u = x * NT + tid, per_row = a.H * upr, j = u / per_row;
     if (j >= s.n || s.pos0 + j < 0) return;
-    const int v = u - j * per_row, h = v / upr;
+    const int v = u - j * per_row, h = v >> upr_log2;
     const int2 at = unit_columns(v - h * upr, a.rot_dim);
-    const bf16_t* src = qkv + (size_t)j * a.ld_qkv + h * c.DH;
-    float w[16];
-    unpack8(*reinterpret_cast<const uint4*>(src + at.x), w);
-    unpack8(*reinterpret_cast<const uint4*>(src + at.y), w + 8);
-    rotate(w, at, a.rot, a.rot_dim, a.cs + (size_t)(s.pos0 + j) * a.rot_dim);
+    Unit w;
+    w.load(qkv + (size_t)j * a.ld_qkv + h * c.DH, at);
+    rotate<ROT>(w, at, a.rot_dim, a.cs + (size_t)(s.pos0 + j) * a.rot_dim);
     bf16_t* dst = a.q[g] + (size_t)(s.row0 + j) * a.ld_q + h * c.DH;
-    *reinterpret_cast<uint4*>(dst + at.x) = make_uint4(pack2(w[0], w[1]), pack2(w[2], w[3]), pack2(w[4], w[5]), pack2(w[6], w[7]));
-    *reinterpret_cast<uint4*>(dst + at.y) = make_uint4(pack2(w[8], w[9]), pack2(w[10], w[11]), pack2(w[12], w[13]), pack2(w[14], w[15]));
+    *reinterpret_cast<uint4*>(dst + at.x) = make_uint4(pack2(w.x[0], w.x[1]), pack2(w.x[2], w.x[3]), pack2(w.x[4], w.x[5]), pack2(w.x[6], w.x[7]));
+    *reinterpret_cast<uint4*>(dst + at.y) = make_uint4(pack2(w.x[8], w.x[9]), pack2(w.x[10], w.x[11]), pack2(w.x[12], w.x[13]), pack2(w.x[14], w.x[15]));
     return;
   }
   const int per_page = 2 * c.HKV, nth = x / per_page, hv = x - nth * per_page, h = hv >> 1, is_v = hv & 1;
@@ -133,21 +132,19 @@ __global__ __launch_bounds__(NT) void append_kernel(const AppendArgs a) {
   const float before = fresh ? 0.f : *scale;
   const bf16_t* const src = qkv + (size_t)(a.H + (is_v ? c.HKV : 0) + h) * c.DH;
   const int units = (hi - lo) * upr;
-  float w[UPT][16];
+  Unit w[UPT];
+#pragma unroll
+  for (int i = 0; i < UPT; ++i) {  // every load before the first use; a row past the last one is that one again
+    const int u = min(i * NT + tid, units - 1), r = u >> upr_log2;
+    w[i].load(src + (size_t)(lo + r - s.pos0) * a.ld_qkv, unit_columns(u - r * upr, a.rot_dim));
+  }
   float most = 0.f;
 #pragma unroll
   for (int i = 0; i < UPT; ++i) {
-    const int u = i * NT + tid;
-    if (u < units) {
-      const int r = u / upr, pos = lo + r;
-      const int2 at = unit_columns(u - r * upr, a.rot_dim);
-      const bf16_t* row = src + (size_t)(pos - s.pos0) * a.ld_qkv;
-      unpack8(*reinterpret_cast<const uint4*>(row + at.x), w[i]);
-      unpack8(*reinterpret_cast<const uint4*>(row + at.y), w[i] + 8);
-      if (!is_v) rotate(w[i], at, a.rot, a.rot_dim, a.cs + (size_t)pos * a.rot_dim);
+    const int u = min(i * NT + tid, units - 1), r = u >> upr_log2;
+    if (!is_v) rotate<ROT>(w[i], unit_columns(u - r * upr, a.rot_dim), a.rot_dim, a.cs + (size_t)(lo + r) * a.rot_dim);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) most = fmaxf(most, fabsf(w[i][e]) <= FLT_MAX ? fabsf(w[i][e]) : 0.f);
-    }
+    for (int e = 0; e < 16; ++e) most = fmaxf(most, fabsf(w[i].x[e]) <= FLT_MAX ? fabsf(w[i].x[e]) : 0.f);
   }
   most = wave_max(most);
   if (NT > 64) {
@@ -164,9 +161,7 @@ __global__ __launch_bounds__(NT) void append_kernel(const AppendArgs a) {
     uint4* p = reinterpret_cast<uint4*>(codes);
     for (int i = tid; i < (lo - page0) * c.DH / 16; i += NT) {
       const uint4 old = p[i];
-      float y[16];
-      from_codes<KIND>(old.x, y), from_codes<KIND>(old.y, y + 4), from_codes<KIND>(old.z, y + 8), from_codes<KIND>(old.w, y + 12);
-      p[i] = make_uint4(to_codes<KIND>(y, f), to_codes<KIND>(y + 4, f), to_codes<KIND>(y + 8, f), to_codes<KIND>(y + 12, f));
+      p[i] = make_uint4(again<KIND>(old.x, f), again<KIND>(old.y, f), again<KIND>(old.z, f), again<KIND>(old.w, f));
     }
   }
   const float by = 1.0f / now;
@@ -174,22 +169,29 @@ __global__ __launch_bounds__(NT) void append_kernel(const AppendArgs a) {
   for (int i = 0; i < UPT; ++i) {
     const int u = i * NT + tid;
     if (u < units) {
-      const int r = u / upr;
+      const int r = u >> upr_log2;
       const int2 at = unit_columns(u - r * upr, a.rot_dim);
       uint8_t* row = codes + (size_t)(lo - page0 + r) * c.DH;
-      *reinterpret_cast<uint2*>(row + at.x) = make_uint2(to_codes<KIND>(w[i], by), to_codes<KIND>(w[i] + 4, by));
-      *reinterpret_cast<uint2*>(row + at.y) = make_uint2(to_codes<KIND>(w[i] + 8, by), to_codes<KIND>(w[i] + 12, by));
+      const float* x = w[i].x;
+      *reinterpret_cast<uint2*>(row + at.x) = make_uint2(to_codes<KIND>(x[0], x[1], x[2], x[3], by), to_codes<KIND>(x[4], x[5], x[6], x[7], by));
+      *reinterpret_cast<uint2*>(row + at.y) = make_uint2(to_codes<KIND>(x[8], x[9], x[10], x[11], by), to_codes<KIND>(x[12], x[13], x[14], x[15], by));
     }
   }
   if (tid == 0) *scale = now;
 }
 
+template <int KIND, int ROT>
+void run_append(const AppendArgs& a, dim3 grid, int nt, int upt, hipStream_t s) {
+  if (nt == 64) hipLaunchKernelGGL((append_kernel<KIND, ROT, 64, 1>), grid, dim3(64), 0, s, a);
+  else if (upt == 1) hipLaunchKernelGGL((append_kernel<KIND, ROT, 256, 1>), grid, dim3(256), 0, s, a);
+  else if (upt == 2) hipLaunchKernelGGL((append_kernel<KIND, ROT, 256, 2>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((append_kernel<KIND, ROT, 256, 4>), grid, dim3(256), 0, s, a);
+}
 template <int KIND>
 void run_append(const AppendArgs& a, dim3 grid, int nt, int upt, hipStream_t s) {
-  if (nt == 64) hipLaunchKernelGGL((append_kernel<KIND, 64, 1>), grid, dim3(64), 0, s, a);
-  else if (upt == 1) hipLaunchKernelGGL((append_kernel<KIND, 256, 1>), grid, dim3(256), 0, s, a);
-  else if (upt == 2) hipLaunchKernelGGL((append_kernel<KIND, 256, 2>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((append_kernel<KIND, 256, 4>), grid, dim3(256), 0, s, a);
+  if (a.rot == ROT_HALVES) run_append<KIND, ROT_HALVES>(a, grid, nt, upt, s);
+  else if (a.rot == ROT_NEIGHBOURS) run_append<KIND, ROT_NEIGHBOURS>(a, grid, nt, upt, s);
+  else run_append<KIND, ROT_NONE>(a, grid, nt, upt, s);
 }
 
 }  // namespace
@@ -225,7 +227,7 @@ const char* append_refusal(const AppendArgs& a) {
   if (a.rot != ROT_NONE && a.rot != ROT_HALVES && a.rot != ROT_NEIGHBOURS) return "unknown rotation";
   if (a.rot != ROT_NONE) {
     if (a.rot_dim < 16 || a.rot_dim > c.DH || a.rot_dim % 16) return "rot_dim is a multiple of 16 up to the head width";
-    if (!a.cs) return "a rotation needs its table";
+    if (!a.cs || (uintptr_t)a.cs % 16) return "a rotation needs its table, 16-byte aligned";
   }
   for (int g = 0; g < c.G; ++g) {
     if (!a.qkv[g] || (uintptr_t)a.qkv[g] % 16) return "qkv is NULL or not 16-byte aligned";

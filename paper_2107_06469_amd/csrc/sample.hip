@@ -6,12 +6,13 @@
 //     (In log2 throughout: a factor and a constant that all scores share change nothing.)
 //   T <= 0: the largest logit.  logprob = z_token - log sum_i exp z_i over all tokens, at temperature 1.
 //   A logit of -inf or NaN is never drawn, +inf counts as the largest float; without a token that can be drawn: -1 and -inf.
-// A row is one workgroup's, its first 128 KB wait in LDS between the passes.  A histogram over the range of logits in question finds where the
-// count or the sum of w is reached: 2048 bins hold a count and the sum of w over the bin's largest possible w, in fixed point (2^-26), so that no
-// order of additions matters.  Usually few tokens stand before the end of that bin: they go to a list, which is sorted, and what is left of
-// the three rules and the draw look at nothing else.  Otherwise the bin is the next round's range, until its tokens fit a list of 256 that is ranked
-// directly (equal logits are told apart by histograms over their indices), and the draw goes over the row once more.
+// A row is one workgroup's, its first 127 KB wait in LDS between the passes.  A histogram over the range of logits finds where the count or the
+// sum of w is reached: 2048 bins hold a count and the sum of w over the bin's largest possible w, in fixed point (2^-26), so that no order of
+// additions matters.  Usually at most 4096 tokens stand before the end of that bin: their indices go to a list, and what is left of the rules
+// and the draw look at nothing else.  Up to 128 of them are ranked directly; of more, or over the whole row, the bin is the next round's range
+// until 256 tokens at most are left in it (equal logits are told apart by histograms over their indices).
 #include <float.h>
+#include <type_traits>
 
 #include "kernels.h"
 #include "wave_math.h"
@@ -19,8 +20,8 @@
 namespace hydra {
 namespace {
 
-constexpr int NT = 1024, NB = 2048, CAP = 256, LIST = 2048;
-constexpr int ROW_BYTES = 131072;  // of a row in LDS
+constexpr int NT = 1024, NB = 2048, CAP = 256, FEW = 128, LIST = 4096;
+constexpr int ROW_BYTES = 130048;  // of a row in LDS
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_INF = -__builtin_inff();
@@ -45,21 +46,20 @@ __device__ __forceinline__ float key_logit(u64 k) {
 __device__ __forceinline__ int key_index(u64 k) { return (int)(0xffffffffu - (unsigned)k); }
 
 struct Shared {
-  union {
-    u64 bin[NB];      // count << 45 | sum of w / (largest w of the bin), 2^-26
-    u64 list[LIST];   // order keys
-    struct { u64 key[CAP], w[CAP]; } some;
-  };
-  float part_a[NT / 64];
+  u64 bin[NB];      // count << 45 | sum of w / (largest w of the bin), 2^-26
+  unsigned list[LIST];
+  float part_a[NT / 64], part_b[NT / 64], part_z[NT / 64];
   int part_i[NT / 64];
   unsigned part_n[NT / 64];
-  u64 part_w[NT / 64];
-  int n, at, found_i;
+  double part_w[NT / 64];
+  int n, at, odd, found_i;
   unsigned above_n, here_n;
-  u64 above_w, run_w;
+  double above_w, run_w;
   float found_z;
-  float best_z;
 };
+// up to CAP tokens that are ranked, in the bins' place
+struct Some { u64 key[CAP], w[CAP]; };
+static_assert(sizeof(Some) <= NB * sizeof(u64), "the ranked tokens take the bins' place");
 
 // The row's tokens, 16 bytes at a time: those in LDS, then those that are read again.
 template <typename T>
@@ -68,7 +68,7 @@ struct Row {
   const T* p;
   uint4* lds;
   int V, n_vec, n_lds;  // tokens; runs of VEC of them, the last one perhaps in part; runs in LDS
-  bool wide, odd;       // 16-byte loads; some logit is NaN or +inf
+  bool wide, odd;       // 16-byte loads; some logit, or the rest of the last run, is no finite number
   __device__ __forceinline__ uint4 load(int q) const {
     if (wide && (q + 1) * VEC <= V) return *reinterpret_cast<const uint4*>(p + (size_t)q * VEC);
     uint32_t w[4];
@@ -81,6 +81,10 @@ struct Row {
         w[e] = (q * 8 + 2 * e < V ? (uint32_t)p[q * 8 + 2 * e] : 0xff80u) | (q * 8 + 2 * e + 1 < V ? (uint32_t)p[q * 8 + 2 * e + 1] : 0xff80u) << 16;
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (VEC == 4) return logit(i < n_lds * VEC ? reinterpret_cast<const float*>(lds)[i] : p[i]);
+    else return logit(__uint_as_float((uint32_t)(i < n_lds * VEC ? reinterpret_cast<const bf16_t*>(lds)[i] : p[i]) << 16));
   }
   template <bool FIX, typename F>
   static __device__ __forceinline__ void tokens(const uint4& v, int q, F& f) {
@@ -97,23 +101,29 @@ struct Row {
       }
     }
   }
-  // Every token once: f(logit, index).  Tokens past the row's end are -inf.  Four loads from memory are under way together.
+  // Every run once: f(fix, run, number), fix false where all logits are finite.  Four loads from memory are under way together.
   template <bool FIX, typename F>
   __device__ __forceinline__ void all(F& f) const {
-    for (int q = threadIdx.x; q < n_lds; q += NT) tokens<FIX>(lds[q], q, f);
+    constexpr std::integral_constant<bool, FIX> fix{};
+    for (int q = threadIdx.x; q < n_lds; q += NT) f(fix, lds[q], q);
     for (int q0 = n_lds + threadIdx.x; q0 < n_vec; q0 += 4 * NT) {
       uint4 v[4];
 #pragma unroll
       for (int s = 0; s < 4; ++s) v[s] = q0 + s * NT < n_vec ? load(q0 + s * NT) : make_uint4(0, 0, 0, 0);
 #pragma unroll
       for (int s = 0; s < 4; ++s)
-        if (q0 + s * NT < n_vec) tokens<FIX>(v[s], q0 + s * NT, f);
+        if (q0 + s * NT < n_vec) f(fix, v[s], q0 + s * NT);
     }
   }
   template <typename F>
-  __device__ __forceinline__ void each(F f) const {
+  __device__ __forceinline__ void runs(F f) const {
     if (odd) all<true>(f);
     else all<false>(f);
+  }
+  // The same by tokens: f(logit, index); tokens past the row's end are -inf.
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    runs([&](auto fix, const uint4& v, int q) { tokens<decltype(fix)::value>(v, q, f); });
   }
   // The first pass: what LDS holds goes there; f as in all(), with the logits as they are.
   template <typename F>
@@ -132,6 +142,18 @@ struct Row {
   }
 };
 
+// The listed tokens of a row.
+template <typename T>
+struct Listed {
+  const Row<T>& row;
+  const unsigned* list;
+  int n;
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    for (int e = threadIdx.x; e < n; e += NT) f(row.at((int)list[e]), (int)list[e]);
+  }
+};
+
 __device__ __forceinline__ float block_max(float v, float* part) {
   v = wave_max(v);
   __syncthreads();
@@ -139,35 +161,30 @@ __device__ __forceinline__ float block_max(float v, float* part) {
   __syncthreads();
   return wave_max(part[threadIdx.x & (NT / 64 - 1)]);
 }
-__device__ __forceinline__ float block_sum(float v, float* part) {
-  v = wave_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float r = part[0];
-#pragma unroll
-  for (int i = 1; i < NT / 64; ++i) r += part[i];
-  return r;
-}
-__device__ __forceinline__ u64 fixed(float w) { return (u64)(w * 17592186044416.f); }  // 2^44
+// Sums of weights do not depend on their order: a token's weight is a whole number of 2^-44, a bin's one of 2^-34 (of which a double holds 2^19
+// exactly, and all tokens together weigh 2^18 at most).
+__device__ __forceinline__ u64 fixed(float w) { return (u64)(w * 17592186044416.f); }
+__device__ __forceinline__ double bin_units(u64 w) { return (double)w * (1.0 / 1024.0); }
+constexpr double BIN_ONE = 17179869184.0;
 
-// Sums of everything up to and with this thread's (n, w), in thread order; total: over all threads.
-__device__ __forceinline__ void block_scan(unsigned& n, u64& w, unsigned& total_n, u64& total_w, Shared& sh) {
+// In thread order: the sums of (n, w) before this thread's, and the sum of all w.
+__device__ __forceinline__ void block_scan(unsigned n, double w, unsigned& before_n, double& before_w, double& all_w, Shared& sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const unsigned pn = __shfl_up(n, d);
-    const u64 pw = __shfl_up(w, d);
+    const double pw = __shfl_up(w, d);
     if (lane >= d) n += pn, w += pw;
   }
-  __syncthreads();
   if (lane == 63) sh.part_n[wave] = n, sh.part_w[wave] = w;
+  before_n = __shfl_up(n, 1), before_w = __shfl_up(w, 1);
+  if (!lane) before_n = 0, before_w = 0;
   __syncthreads();
-  total_n = 0, total_w = 0;
+  all_w = 0;
 #pragma unroll
   for (int i = 0; i < NT / 64; ++i) {
-    if (i == wave) n += total_n, w += total_w;
-    total_n += sh.part_n[i], total_w += sh.part_w[i];
+    if (i < wave) before_n += sh.part_n[i], before_w += sh.part_w[i];
+    all_w += sh.part_w[i];
   }
 }
 
@@ -185,76 +202,76 @@ struct Range {
   __device__ __forceinline__ bool in(const Last& t, float z, int i) const {
     return z <= hi && z >= lo && kept(t, z, i) && (!ties || (i >= i_lo && i < i_lo + i_n));
   }
-  // the largest logit is alone in the first bin, so that every round takes something out of the next one's range
+  // after the first round the largest logit is alone in the first bin, so that every round takes something out of the next one's range
+  bool first;
   __device__ __forceinline__ int bin_of(float z, int i) const {
-    return ties ? (int)((unsigned)(i - i_lo) / per) : z == hi ? 0 : (int)fminf(fmaxf((hi - z) * c, 1.f), (float)(NB - 1));
+    return ties ? (int)((unsigned)(i - i_lo) / per) : (int)fminf(fmaxf((hi - z) * c, first || z == hi ? 0.f : 1.f), (float)(NB - 1));
   }
 };
 __device__ __forceinline__ void clear(Shared& sh) {
-  __syncthreads();
-  for (int i = threadIdx.x; i < NB; i += NT) sh.bin[i] = 0;
-  if (threadIdx.x == 0) sh.n = 0, sh.at = -1;
-  __syncthreads();
+  for (int i = threadIdx.x; i < NB / 2; i += NT) reinterpret_cast<uint4*>(sh.bin)[i] = make_uint4(0, 0, 0, 0);
+  if (threadIdx.x == 0) sh.at = -1;
 }
 // inv: log2(e) / T; a bin's largest weight is that of its upper edge
 __device__ __forceinline__ float edge(const Range& g, int bin, float zmax, float inv) { return (g.hi - zmax) * inv - (g.ties || !bin ? 0.f : (float)bin * (inv / g.c)); }
-__device__ __forceinline__ u64 entry(const Range& g, int bin, float z, float zmax, float inv, bool mass) {
-  constexpr u64 ONE = 1ull << 45;
-  if (!mass) return ONE;
-  return ONE + (u64)(unsigned)(fminf(exp2_hw((z - zmax) * inv - edge(g, bin, zmax, inv)), 2.f) * 67108864.f);
-}
-// sh.at: the first bin through which the sum of counts (by_mass: of weights) reaches k (p times `of`, or times the sum of all bins where `of` is 0);
-// -1 where none does.  sh.above_*: the sums before it; sh.here_n: its count; returns the target that the sum of weights was held against.
-__device__ __forceinline__ u64 find_bin(const Range& g, Shared& sh, float zmax, float inv, bool mass, bool by_mass, unsigned k, u64 target, float p) {
-  const int b = 2 * (int)threadIdx.x;
+// sh.at: the first bin through which the sum of counts (by_mass: of weights) reaches k (the target; with p >= 0 that is p times the sum of all bins);
+// it stays -1 where none does.  sh.above_*: the sums before it; sh.here_n: its count; returns the target.
+__device__ __forceinline__ double find_bin(const Range& g, Shared& sh, float zmax, float inv, bool mass, bool by_mass, unsigned k, double target, float p, double& total) {
+  constexpr int PER = NB / NT;
+  const int b = PER * (int)threadIdx.x;
   __syncthreads();
-  const u64 e0 = sh.bin[b], e1 = sh.bin[b + 1];
-  const unsigned n0 = (unsigned)(e0 >> 45), n1 = (unsigned)(e1 >> 45);
-  u64 w0 = 0, w1 = 0;
-  if (mass) {
-    constexpr double UNIT = 262144.;  // 2^44 / 2^26
-    constexpr u64 LOW = (1ull << 45) - 1;
-    w0 = (u64)((double)(e0 & LOW) * ((double)exp2_hw(edge(g, b, zmax, inv)) * UNIT));
-    w1 = (u64)((double)(e1 & LOW) * ((double)exp2_hw(edge(g, b + 1, zmax, inv)) * UNIT));
+  unsigned n[PER], all_n = 0;
+  double w[PER], all_w = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const u64 e = sh.bin[b + i];
+    n[i] = (unsigned)(e >> 45);
+    w[i] = 0;
+    if (mass && n[i])  // two conversions: the sum has 45 bits
+      w[i] = rint(((double)((unsigned)(e >> 32) & 0x1fffu) * 4294967296.0 + (double)(unsigned)e) *
+                  ((double)exp2_hw(edge(g, b + i, zmax, inv)) * (BIN_ONE / 67108864.0)));
+    all_n += n[i], all_w += w[i];
   }
-  unsigned n = n0 + n1, all_n;
-  u64 w = w0 + w1, all_w;
+  unsigned cn;
+  double cw;
   const unsigned an = sh.above_n;
-  const u64 aw = sh.above_w;
-  block_scan(n, w, all_n, all_w, sh);
-  if (p >= 0.f) {
-    const double want = __builtin_ceil((double)p * (double)all_w);
-    target = want < 1.0 ? 1ull : (u64)want;
+  const double aw = sh.above_w;
+  block_scan(all_n, all_w, cn, cw, total, sh);
+  if (p >= 0.f) target = (double)p * total;
+  cn += an, cw += aw;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const unsigned nn = cn + n[i];
+    const double nw = cw + w[i];
+    if (by_mass ? cw < target && nw >= target : cn < k && nn >= k) sh.at = b + i, sh.above_n = cn, sh.above_w = cw, sh.here_n = n[i];
+    cn = nn, cw = nw;
   }
-  n += an, w += aw;
-  // sums through the end of bin b, and through b + 1
-  const unsigned na = n - n1;
-  const u64 wa = w - w1;
-  const bool here0 = by_mass ? wa - w0 < target && wa >= target : na - n0 < k && na >= k;
-  const bool here1 = by_mass ? wa < target && w >= target : na < k && n >= k;
-  if (here0) sh.at = b, sh.above_n = na - n0, sh.above_w = wa - w0, sh.here_n = n0;
-  if (here1) sh.at = b + 1, sh.above_n = na, sh.above_w = wa, sh.here_n = n1;
   __syncthreads();
   return target;
 }
 
 // The last token of the run that reaches k tokens, or the mass `target`, among those kept by `t`; t itself where nothing does.  begun: the first
-// round's histogram stands in sh and find_bin has been called.  sh.run_w: the run's mass, where it is found (sh.found_i >= 0).
+// round's histogram has been taken and find_bin called.  sh.run_w: the run's mass, where it is found (sh.found_i >= 0).
 template <typename R>
-__device__ __forceinline__ Last find_last(const R& row, Shared& sh, Range g, bool begun, Last t, float zmax, float inv, bool by_mass, unsigned k, u64 target,
+__device__ __forceinline__ Last find_last(const R& row, Shared& sh, Range g, bool begun, Last t, float zmax, float inv, bool by_mass, unsigned k, double target,
                                           bool mass) {
   const int tid = threadIdx.x;
+  Some& some = *reinterpret_cast<Some*>(sh.bin);
   while (true) {
     if (!begun) {
       g.begin();
+      __syncthreads();
       clear(sh);
+      __syncthreads();
       row.each([&](float z, int i) {
         if (g.in(t, z, i)) {
           const int bin = g.bin_of(z, i);
-          atomicAdd(&sh.bin[bin], entry(g, bin, z, zmax, inv, mass));
+          const unsigned w = mass ? (unsigned)(fminf(exp2_hw((z - zmax) * inv - edge(g, bin, zmax, inv)), 2.f) * 67108864.f) : 0u;
+          atomicAdd(&sh.bin[bin], (u64)w | 1ull << 45);
         }
       });
-      find_bin(g, sh, zmax, inv, mass, by_mass, k, target, -1.f);
+      double all_w;
+      find_bin(g, sh, zmax, inv, mass, by_mass, k, target, -1.f, all_w);
     }
     begun = false;
     const int bin = sh.at;
@@ -266,17 +283,24 @@ __device__ __forceinline__ Last find_last(const R& row, Shared& sh, Range g, boo
       row.each([&](float z, int i) {
         if (g.in(t, z, i) && g.bin_of(z, i) == bin) {
           const int at = atomicAdd(&sh.n, 1);
-          if (at < CAP) sh.some.key[at] = order_key(z, i), sh.some.w[at] = mass ? fixed(exp2_hw((z - zmax) * inv)) : 0;
+          if (at < CAP) some.key[at] = order_key(z, i), some.w[at] = mass ? fixed(exp2_hw((z - zmax) * inv)) : 0;
         }
       });
       __syncthreads();
       if (tid < (int)n) {
-        const u64 key = sh.some.key[tid], own = sh.some.w[tid];
-        unsigned before = sh.above_n;
-        u64 w = sh.above_w;
-        for (unsigned q = 0; q < n; ++q)
-          if (sh.some.key[q] > key) ++before, w += sh.some.w[q];
-        if (by_mass ? w < target && w + own >= target : before == k - 1) sh.found_z = key_logit(key), sh.found_i = key_index(key), sh.run_w = w + own;
+        const u64 key = some.key[tid], own = some.w[tid];
+        unsigned before = sh.above_n, last = 0;
+        u64 w = 0;
+#pragma unroll 4
+        for (unsigned q = 0; q < n; ++q) {
+          const u64 other = some.key[q], weight = some.w[q];
+          if (other > key) ++before, w += weight;
+          last += other < key;
+        }
+        // (the bin's own sum has reached the target, so its last token has)
+        const double cw = sh.above_w + bin_units(w), nw = sh.above_w + bin_units(w + own);
+        if (by_mass ? (cw < target || before == sh.above_n) && (nw >= target || !last) : before == k - 1)
+          sh.found_z = key_logit(key), sh.found_i = key_index(key), sh.run_w = nw;
       }
       __syncthreads();
       return sh.found_i < 0 ? t : Last{sh.found_z, sh.found_i};
@@ -291,31 +315,67 @@ __device__ __forceinline__ Last find_last(const R& row, Shared& sh, Range g, boo
     });
     g.hi = block_max(most, sh.part_a);
     g.lo = g.low = -block_max(least, sh.part_a);
-    g.ties = g.hi == g.lo;
+    g.ties = g.hi == g.lo, g.first = false;
   }
 }
 
-// Larger keys first.  n keys, room for the next power of two.
-__device__ __forceinline__ void sort_keys(u64* key, int n) {
-  int m = 64;
-  while (m < n) m <<= 1;
-  for (int i = n + (int)threadIdx.x; i < m; i += NT) key[i] = 0;
-  for (int k = 2; k <= m; k <<= 1)
-    for (int j = k >> 1; j; j >>= 1) {
-      __syncthreads();
-      for (int p = threadIdx.x; p < m / 2; p += NT) {
-        const int a = (p & ~(j - 1)) * 2 | (p & (j - 1)), b = a | j;  // the pair whose numbers differ in j
-        const u64 x = key[a], y = key[b];
-        if ((x < y) == !(a & k)) key[a] = y, key[b] = x;
+struct Best { float s, z; int i; };
+__device__ __forceinline__ void race(Best& b, float z, int i, float zmax, float inv, float u) {
+  const float s = fmaxf((z - zmax) * inv - __builtin_amdgcn_logf(-__builtin_amdgcn_logf(fminf(u, 0.99999994f))), -FLT_MAX);
+  if (s > b.s || (s == b.s && i < b.i)) b = {s, z, i};
+}
+// f(logit, index, uniform) for the tokens of every run of 16 bytes whose largest logit `maybe` takes.  The uniforms of four runs are
+// asked for together: a load each, behind its own test, would be waited for one by one.
+template <typename T, bool FIX, typename M, typename F>
+__device__ __forceinline__ void with_uniforms(const Row<T>& row, const float* u, M maybe, F f) {
+  constexpr int VEC = Row<T>::VEC;
+  const bool wide = (uintptr_t)u % 16 == 0;
+  for (int q0 = threadIdx.x; q0 < row.n_vec; q0 += 4 * NT) {
+    uint4 v[4];
+    float4 w[4][VEC / 4];
+    bool some[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int q = q0 + s * NT;
+      some[s] = q < row.n_vec;
+      if (some[s]) v[s] = q < row.n_lds ? row.lds[q] : row.load(q);
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int first = (q0 + s * NT) * VEC;
+      float most = NEG_INF;
+      auto up = [&](float z, int) { most = fmaxf(most, z); };
+      if (some[s]) Row<T>::template tokens<FIX>(v[s], 0, up);
+      some[s] = some[s] && maybe(most);
+      if (some[s]) {
+        if (wide && first + VEC <= row.V) {
+#pragma unroll
+          for (int e = 0; e < VEC / 4; ++e) w[s][e] = *reinterpret_cast<const float4*>(u + first + 4 * e);
+        } else {
+          float x[VEC];
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) x[e] = u[min(first + e, row.V - 1)];
+#pragma unroll
+          for (int e = 0; e < VEC / 4; ++e) w[s][e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+        }
       }
     }
-  __syncthreads();
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      if (some[s]) {
+        const int first = (q0 + s * NT) * VEC;
+        auto one = [&](float z, int e) {
+          const float4 x = w[s][e >> 2];
+          f(z, first + e, (e & 3) == 0 ? x.x : (e & 3) == 1 ? x.y : (e & 3) == 2 ? x.z : x.w);
+        };
+        Row<T>::template tokens<FIX>(v[s], 0, one);
+      }
+  }
 }
-
-struct Best { float s, z; int i; };
-__device__ __forceinline__ void race(Best& b, float z, int i, float zmax, float inv, const float* u) {
-  const float s = fmaxf((z - zmax) * inv - __builtin_amdgcn_logf(-__builtin_amdgcn_logf(fminf(u[i], 0.99999994f))), -FLT_MAX);
-  if (s > b.s || (s == b.s && i < b.i)) b = {s, z, i};
+template <typename T, typename M, typename F>
+__device__ __forceinline__ void race_pass(const Row<T>& row, const float* u, M maybe, F f) {
+  if (row.odd) with_uniforms<T, true>(row, u, maybe, f);
+  else with_uniforms<T, false>(row, u, maybe, f);
 }
 
 template <typename T>
@@ -333,17 +393,18 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
   const float temp = a.temperature[r], top_p = a.top_p[r], min_p = fminf(a.min_p[r], 1.f);
   const int top_k = a.top_k[r];
   const bool greedy = !(temp > 0.f);
+  clear(sh);
+  if (tid == 0) sh.n = 0, sh.odd = 0, sh.above_n = 0, sh.above_w = 0;
   float most = NEG_INF;
   bool odd = false;
   row.first([&](float z, int) {
     most = fmaxf(most, z);
-    odd |= !(z <= FLT_MAX);
+    odd |= !(fabsf(z) <= FLT_MAX);
   });
-  if (tid == 0) sh.n = 0, sh.above_n = 0, sh.above_w = 0;
   const float zmax = fminf(block_max(most, sh.part_a), FLT_MAX);
-  if (odd) sh.n = 1;
+  if (odd) sh.odd = 1;
   __syncthreads();
-  row.odd = sh.n;
+  row.odd = sh.odd;
   if (zmax == NEG_INF) {
     if (tid == 0) {
       a.token[g][r] = -1;
@@ -357,99 +418,153 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
   const bool want_lse = a.logprob[g] != nullptr;
   float lse = 0.f;
   Best best = {NEG_INF, NEG_INF, 0x7fffffff};
-  if (!by_k && !by_p) {  // one pass
+  auto heavy = [&](float z) { return min_p <= 0.f || exp2_hw((z - zmax) * inv) >= min_p; };
+  if (greedy) {
     row.each([&](float z, int i) {
       if (want_lse) lse += exp2_hw((z - zmax) * LOG2E);
-      if (greedy ? z == zmax && i < best.i : z > NEG_INF && (min_p <= 0.f || exp2_hw((z - zmax) * inv) >= min_p)) {
-        if (greedy) best = {0.f, z, i};
-        else race(best, z, i, zmax, inv, u);
-      }
+      if (z == zmax && i < best.i) best = {0.f, z, i};
+    });
+  } else if (!by_k && !by_p) {
+    if (want_lse) row.each([&](float z, int) { lse += exp2_hw((z - zmax) * LOG2E); });
+    race_pass(row, u, [&](float z) { return z > NEG_INF && heavy(z); }, [&](float z, int i, float x) {
+      if (z > NEG_INF && heavy(z)) race(best, z, i, zmax, inv, x);
     });
   } else {
-    Range range = {zmax, -FLT_MAX, fmaxf(zmax - DEPTH / inv, -FLT_MAX), false, 0, a.V, 0.f, 0};
+    // the first round, over all tokens that can be drawn
+    Range range = {zmax, -FLT_MAX, fmaxf(zmax - DEPTH / inv, -FLT_MAX), false, 0, a.V, 0.f, 0, true};
     range.begin();
-    clear(sh);
-    row.each([&](float z, int i) {
-      if (want_lse) lse += exp2_hw((z - zmax) * LOG2E);
-      if (z > NEG_INF) {
-        const int bin = range.bin_of(z, i);
-        atomicAdd(&sh.bin[bin], entry(range, bin, z, zmax, inv, by_p));
-      }
-    });
+    const float step = inv / range.c;  // log2 of the weights of two edges
+    const bool lse_here = want_lse && !(by_p && inv == LOG2E);  // at temperature 1 it is the sum of all weights
+    auto count = [&](auto mass, auto more) {
+      row.runs([&](auto fix, const uint4& v, int q) {
+        auto one = [&](float z, int) {
+          const float d = zmax - z, t = d * range.c, bin = truncf(fminf(t, (float)(NB - 1)));
+          if constexpr (more) lse += exp2_hw(d * -LOG2E);
+          const unsigned w = mass ? (unsigned)fminf(exp2_hw(fmaf(bin - t, step, 26.f)), 134217728.f) : 0u;
+          if (!decltype(fix)::value || z > NEG_INF) atomicAdd(&sh.bin[(int)bin], (u64)w | 1ull << 45);
+        };
+        Row<T>::template tokens<decltype(fix)::value>(v, q, one);
+      });
+    };
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+    if (by_p) {
+      if (lse_here) count(yes, yes);
+      else count(yes, no);
+    } else {
+      if (lse_here) count(no, yes);
+      else count(no, no);
+    }
     // both rules end at or before where the first one does: the k-th token, or without top-k the share of all mass
-    u64 target = find_bin(range, sh, zmax, inv, by_p, !by_k, (unsigned)top_k, 0, by_k ? -1.f : fmaxf(top_p, 0.f));
-    const unsigned n = sh.at >= 0 ? sh.above_n + sh.here_n : LIST + 1;
-    if (n <= LIST) {
-      const int bin = sh.at;
+    const bool both = by_k && by_p;
+    const float p = fmaxf(top_p, 1e-30f);
+    double all_w;
+    double target = find_bin(range, sh, zmax, inv, by_p, !by_k, (unsigned)top_k, 0, by_k ? -1.f : p, all_w);
+    if (want_lse && !lse_here && tid == 0) lse = (float)(all_w * (1.0 / BIN_ONE));
+    const unsigned n = sh.at < 0 ? LIST + 1 : sh.above_n + sh.here_n;
+    auto rest = [&](const auto& tokens) {  // the rules that are left, over tokens that hold all that they can keep
+      Last t = find_last(tokens, sh, range, true, Last{-FLT_MAX, 0x7fffffff}, zmax, inv, !by_k, (unsigned)top_k, target, by_p);
+      if (!both) return t;
+      double total = sh.run_w;
+      if (sh.found_i < 0) {  // fewer than k tokens can be drawn: all of them are kept
+        double w = 0, x_w;
+        unsigned x_n;
+        tokens.each([&](float z, int) { w += (double)exp2_hw((z - zmax) * inv); });
+        __syncthreads();
+        block_scan(0, w * BIN_ONE, x_n, x_w, total, sh);
+      }
       __syncthreads();
-      row.each([&](float z, int i) {
-        if (z > NEG_INF && range.bin_of(z, i) <= bin) {
-          const int at = atomicAdd(&sh.n, 1);
-          if (at < LIST) sh.list[at] = order_key(z, i);
+      if (tid == 0) sh.above_n = 0, sh.above_w = 0;
+      return find_last(tokens, sh, range, false, t, zmax, inv, true, 0, p * total, true);
+    };
+    if (n <= LIST) {
+      const float to = (float)(sh.at + 1);
+      const bool any = sh.at == NB - 1;
+      row.runs([&](auto fix, const uint4& v, int q) {
+        float most = NEG_INF;
+        auto up = [&](float z, int) { most = fmaxf(most, z); };
+        Row<T>::template tokens<decltype(fix)::value>(v, q, up);
+        if (most > NEG_INF && (any || (zmax - most) * range.c < to)) {
+          unsigned mask = 0;
+          auto one = [&](float z, int i) { mask |= z > NEG_INF && (any || (zmax - z) * range.c < to) ? 1u << (i % Row<T>::VEC) : 0u; };
+          Row<T>::template tokens<decltype(fix)::value>(v, 0, one);
+          int at = atomicAdd(&sh.n, __popc(mask));
+          for (; mask; mask &= mask - 1, ++at)
+            if (at < LIST) sh.list[at] = (unsigned)(q * Row<T>::VEC + __ffs(mask) - 1);
         }
       });
-      sort_keys(sh.list, (int)n);
-      unsigned none = 0, x_n;
-      u64 w[2], run = 0, all;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int at = 2 * tid + e;
-        w[e] = at < (int)n && (!by_k || at < top_k) ? fixed(exp2_hw((key_logit(sh.list[at]) - zmax) * inv)) : 0;
-        run += w[e];
-      }
-      if (by_p) {
-        block_scan(none, run, x_n, all, sh);
-        if (by_k) {
-          const double want = __builtin_ceil((double)fmaxf(top_p, 0.f) * (double)all);
-          target = want < 1.0 ? 1ull : (u64)want;
+      __syncthreads();
+      if (n <= FEW) {
+        Some& some = *reinterpret_cast<Some*>(sh.bin);
+        float z = NEG_INF, x = 0.f;
+        int i = 0, rank = 0;
+        u64 key = 0, own = 0, before = 0;
+        if (tid < (int)n) {
+          i = (int)sh.list[tid], z = row.at(i), x = u[i];
+          key = order_key(z, i), own = fixed(exp2_hw((z - zmax) * inv));
         }
-        run -= w[0] + w[1];
-      }
+        if (tid < FEW) some.key[tid] = key, some.w[tid] = own;  // 0 behind the last one
+        __syncthreads();
+        if (tid < (int)n) {
+          for (unsigned q0 = 0; q0 < n; q0 += 8)  // eight reads under way together
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int at = 2 * tid + e;
-        if (at < (int)n && (!by_k || at < top_k) && (!by_p || run < target)) {
-          const float z = key_logit(sh.list[at]);
-          if (exp2_hw((z - zmax) * inv) >= min_p) race(best, z, key_index(sh.list[at]), zmax, inv, u);
+            for (unsigned q = 0; q < 8; ++q) {
+              const u64 other = some.key[q0 + q], w = some.w[q0 + q];
+              if (other > key) ++rank, before += w;
+            }
+          if (both && rank == top_k - 1) sh.run_w = bin_units(before + own);
         }
-        run += w[e];
+        if (both) {
+          __syncthreads();
+          target = p * sh.run_w;
+        }
+        if (tid < (int)n && (!by_k || rank < top_k) && (!by_p || !rank || bin_units(before) < target) && heavy(z)) race(best, z, i, zmax, inv, x);
+      } else {
+        const Listed<T> listed = {row, sh.list, (int)n};
+        const Last t = rest(listed);
+        for (int e0 = tid; e0 < (int)n; e0 += 4 * NT) {  // four gathers under way together
+          int i[4];
+          float z[4], x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) i[e] = e0 + e * NT < (int)n ? (int)sh.list[e0 + e * NT] : -1;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[e] = i[e] >= 0 ? row.at(i[e]) : NEG_INF, x[e] = i[e] >= 0 ? u[i[e]] : 0.f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (z[e] > NEG_INF && kept(t, z[e], i[e]) && heavy(z[e])) race(best, z[e], i[e], zmax, inv, x[e]);
+        }
       }
     } else {
-      Last t = {-FLT_MAX, 0x7fffffff};
-      t = find_last(row, sh, range, true, t, zmax, inv, !by_k, (unsigned)top_k, target, by_p);
-      if (by_k && by_p) {
-        u64 total = sh.run_w;
-        if (sh.found_i < 0) {  // fewer than k tokens can be drawn: all of them are kept
-          u64 w = 0, x_w;
-          unsigned x = 0, x_n;
-          row.each([&](float z, int) { w += fixed(exp2_hw((z - zmax) * inv)); });
-          block_scan(x, w, x_n, x_w, sh);
-          total = x_w;
-        }
-        const double want = __builtin_ceil((double)fmaxf(top_p, 0.f) * (double)total);
-        __syncthreads();
-        if (tid == 0) sh.above_n = 0, sh.above_w = 0;
-        t = find_last(row, sh, range, false, t, zmax, inv, true, 0, want < 1.0 ? 1ull : (u64)want, true);
-      }
-      row.each([&](float z, int i) {
-        if (z > NEG_INF && kept(t, z, i) && exp2_hw((z - zmax) * inv) >= min_p) race(best, z, i, zmax, inv, u);
+      const Last t = rest(row);
+      race_pass(row, u, [&](float z) { return z >= t.z; }, [&](float z, int i, float x) {
+        if (z > NEG_INF && kept(t, z, i) && heavy(z)) race(best, z, i, zmax, inv, x);
       });
     }
   }
-#pragma unroll
-  for (int d = 32; d; d >>= 1) {
+  auto join = [&](int d) {
     const Best o = {__shfl_xor(best.s, d), __shfl_xor(best.z, d), __shfl_xor(best.i, d)};
     if (o.s > best.s || (o.s == best.s && o.i < best.i)) best = o;
-  }
-  if (want_lse) lse = block_sum(lse, sh.part_a);
+  };
+#pragma unroll
+  for (int d = 32; d; d >>= 1) join(d);
+  lse = wave_sum(lse);
   __syncthreads();
-  if ((tid & 63) == 0) sh.part_a[tid >> 6] = best.s, sh.part_i[tid >> 6] = best.i, sh.part_n[tid >> 6] = __float_as_uint(best.z);
+  if ((tid & 63) == 0) sh.part_a[tid >> 6] = best.s, sh.part_i[tid >> 6] = best.i, sh.part_z[tid >> 6] = best.z, sh.part_b[tid >> 6] = lse;
   __syncthreads();
-  if (tid == 0) {
-    for (int i = 1; i < NT / 64; ++i)
-      if (sh.part_a[i] > best.s || (sh.part_a[i] == best.s && sh.part_i[i] < best.i)) best = {sh.part_a[i], __uint_as_float(sh.part_n[i]), sh.part_i[i]};
-    a.token[g][r] = best.i;
-    if (want_lse) a.logprob[g][r] = best.z - zmax - __builtin_amdgcn_logf(lse) * LN2;
+  if (tid < 64) {
+    constexpr int NW = NT / 64;
+    best = {sh.part_a[tid % NW], sh.part_z[tid % NW], sh.part_i[tid % NW]};
+#pragma unroll
+    for (int d = NW / 2; d; d >>= 1) join(d);
+    if (tid == 0) {
+      a.token[g][r] = best.i;
+      if (want_lse) {
+        lse = 0.f;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) lse += sh.part_b[i];
+        a.logprob[g][r] = best.z - zmax - __builtin_amdgcn_logf(lse) * LN2;
+      }
+    }
   }
 }
 

@@ -529,6 +529,19 @@ def test_sample_filters(torch, ops, V, dtype):
     assert told >= 3 * rows * 0.8
 
 
+@pytest.mark.parametrize("V", [5000, 32000, 100000, 150001, 262144])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("p", [1.0, 0.4, 0.9, 0.999])
+def test_sample_keeps_few_and_many(torch, ops, V, dtype, p):
+    """Kept sets of one token to tens of thousands: every way of finding the last one."""
+    r = np.random.default_rng(V + int(1000 * p))
+    ks = [0, 1, 2, 100, 128, 129, 257, 1000, 2048, 4096, 4097, 9000]
+    z = logits(r, len(ks), V, "ranked").astype(np.float32)
+    u = r.random((len(ks), V), dtype=np.float32)
+    told = check_sample(torch, ops, [z, z * 0.01], [u, u], [0.9] * len(ks), ks, [p] * len(ks), [0.0] * len(ks), dtype)
+    assert told >= len(ks)
+
+
 @pytest.mark.parametrize("V", [500, 20000, 40000])
 def test_sample_of_equal_logits(torch, ops, V):
     """Ties at the edge of the kept: the lower index stays."""
