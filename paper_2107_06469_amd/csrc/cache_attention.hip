@@ -13,6 +13,7 @@
 // A page's scale multiplies scores (keys) or probabilities (values, in units of 2^-15 of the largest scale met so far: f16 then holds weights down
 // to 2^-39 of the largest).
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 #include "wave_math.h"
@@ -95,6 +96,7 @@ struct CacheAttnPlan {
   int n_split, chunk;  // runs of keys, keys in one (a multiple of 128)
   int n_rt;            // 16-row tiles of the sequence with the most rows
   int page_log2;
+  bool prompt;         // many rows: cache_prompt_kernel, n_rt blocks of 256 rows
 };
 
 // Four waves share a run of keys, 32 at a time in turn, each with its own maximum, sum and accumulators; they are joined through LDS.
@@ -284,6 +286,283 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
   }
 }
 
+// ---- many rows of a key/value head ----------------------------------------------------------------------------------------
+// NW waves, 32 rows each, share tiles of 64 keys through LDS, as f16 (row-major, 16-byte chunks XOR-ed by the row so that reads of 16 rows at one
+// chunk and transposing reads both spread over the banks): codes are widened once for all of a workgroup's rows on their way there.  The
+// next tile's codes are in registers while this one's products run; one barrier a tile.  v_mfma_f32_32x32x16_f16:
+//   S^T[t,i] = K Q^T (lane: query l%32; accumulator rows 8q + 4(l/32) + e),  O^T[d,i] += V^T P^T, P from the accumulators as they are, V^T by transposing
+//   LDS reads.  Values carry 2^7 of their page's scale in units of the window's largest, weights 2^15, so that f16 holds small ones.
+// What a window of 512 pages is (id and scales) waits in LDS, too.
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+__device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// XOR term of a row's chunks: 16 rows of 256 bytes (128 bytes) need 16 (8) different terms, and 4 rows in a row must move a group of 4 chunks
+template <int DH>
+__device__ __forceinline__ int swz(int row) {
+  return DH == 128 ? 4 * (row & 3) + ((row >> 2) & 3) : 4 * ((row >> 1) & 1) + ((row >> 2) & 3);
+}
+// Eight keys of one column per lane: rows r and r + 8 .. of the tile, r = row0 + 4(l/32) + {0..3}, by two transposing reads (within 16 lanes, lane j
+// supplies four columns of row j/4 and lane i receives column i of rows 0..3)
+struct ColumnsAt { unsigned a0, a1; };
+template <int DH>
+__device__ __forceinline__ ColumnsAt columns_at(unsigned tile, int col0, int lane) {
+  constexpr int NCH = DH / 8;
+  const int j = lane & 15, grp = lane >> 4, col = col0 + 16 * (grp & 1) + 4 * (j & 3), kc = col >> 3, half = (col >> 2) & 1;
+  const int r0 = 4 * (grp >> 1) + (j >> 2), r1 = r0 + 8;
+  return {tile + (unsigned)((r0 * NCH + (kc ^ swz<DH>(r0))) * 16 + half * 8), tile + (unsigned)((r1 * NCH + (kc ^ swz<DH>(r1))) * 16 + half * 8)};
+}
+__device__ __forceinline__ uint4 read_columns(const ColumnsAt& c, unsigned off) {
+  typedef __attribute__((ext_vector_type(4))) short s16x4;
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(c.a0 + off)));
+  const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(c.a1 + off)));
+  return make_uint4(lo.x, lo.y, hi.x, hi.y);
+}
+__device__ __forceinline__ uint4 times(const uint4& v, uint32_t f) {
+  const f16x2 m = __builtin_bit_cast(f16x2, f);
+  auto one = [&](uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, w) * m); };
+  return make_uint4(one(v.x), one(v.y), one(v.z), one(v.w));
+}
+constexpr int WINDOW = 512;
+template <int DH>
+constexpr int prompt_lds() { return 2 * 2 * 64 * DH * 2 + 3 * WINDOW * 4 + 64; }
+
+// blockIdx: x sequence and key/value head (the blocks of one head run on one XCD where their number is a multiple of 8), y run of keys and row block, the
+// last (longest) row blocks first; z model.
+template <int KIND, int DH, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAttnArgs a, const CacheAttnPlan pl) {
+  constexpr int NT = NW * 64, NCH = DH / 8, NK = DH / 16, NC = DH / 32, BUF = 2 * 64 * NCH;  // chunks of a buffer: K, then V
+  constexpr int LOADS = 2 * 64 * (DH / 16) / NT;                                             // of 16 codes per thread and tile
+  extern __shared__ __attribute__((aligned(256))) uint4 lds[];
+  int* const s_id = reinterpret_cast<int*>(lds + 2 * BUF);
+  float* const s_ks = reinterpret_cast<float*>(s_id + WINDOW);
+  float* const s_vs = s_ks + WINDOW;
+  int* const s_bad = reinterpret_cast<int*>(s_vs + WINDOW);
+  const CacheArgs& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 31, g = lane >> 5;
+  const int gi = blockIdx.z, b = blockIdx.x / c.HKV, h = blockIdx.x - b * c.HKV;
+  const int split = blockIdx.y / pl.n_rt, blk = pl.n_rt - 1 - (blockIdx.y - split * pl.n_rt);
+  const CacheSeq sq = cache_seq(c, b);
+  const int share = a.H / c.HKV, rows = sq.n * share, first = blk * NW * 32;
+  if (first >= rows) return;
+  auto sees_of = [&](int row) { return row < rows ? (a.causal ? max(sq.pos0 + row / share + 1, 0) : sq.len) : 0; };
+  const int row = first + wave * 32 + li, sees = sees_of(row), rc = min(row, rows - 1), j = rc / share, hq = h * share + rc - j * share;
+  const int t_lo = split * pl.chunk, t_hi = min(t_lo + pl.chunk, sees_of(min(first + NW * 32, rows) - 1));
+  const int wave_last = min(first + wave * 32 + 32, rows) - 1, wave_all = first + wave * 32 < rows ? min(sees_of(wave_last), t_hi) : 0;
+  const int wave_free = first + wave * 32 + 32 <= rows ? min(sees_of(first + wave * 32), t_hi) : 0;  // keys that all of the wave's rows see
+
+  uint4 qf[NK];
+  float q_scale;
+  {
+    const bf16_t* q = a.q[gi] + (size_t)(sq.row0 + j) * a.ld_q + (size_t)hq * DH + 8 * g;
+    uint4 raw[NK];
+    float most = 0.f;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) raw[k] = *reinterpret_cast<const uint4*>(q + 16 * k);
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+      const uint32_t v[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(fabsf(__uint_as_float(v[e] << 16)), fabsf(__uint_as_float(v[e] & 0xffff0000u))));
+    }
+    const float2 both = wave_swap32(most);
+    most = fmaxf(both.x, both.y);
+    const unsigned ex = min(max(__float_as_uint(most) >> 23, 1u), 253u);
+    const float f = __uint_as_float((254u - ex) << 23);
+    q_scale = __uint_as_float(ex << 23) * (a.scale * LOG2E);
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+      uint32_t v[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = pack_f16(__uint_as_float(v[e] << 16) * f, __uint_as_float(v[e] & 0xffff0000u) * f);
+      qf[k] = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+  }
+
+  const uint4* kr[NK];
+  ColumnsAt vc[NC];
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char*)reinterpret_cast<const char*>(lds);
+#pragma unroll
+  for (int k = 0; k < NK; ++k) kr[k] = lds + li * NCH + ((2 * k + g) ^ swz<DH>(li));
+#pragma unroll
+  for (int i = 0; i < NC; ++i) vc[i] = columns_at<DH>(lds0 + 64 * NCH * 16, 32 * i, lane);
+
+  f32x16 acc[NC];
+#pragma unroll
+  for (int i = 0; i < NC; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
+  float m = NEG_BIG, l = 0.f, unit = 0.f;
+  int win = 0;       // the window's first page
+  bool bad = false;  // some page of the window is not there
+  auto window = [&](int key) {
+    win = key >> pl.page_log2;
+    __syncthreads();
+    if (tid == 0) *s_bad = 0;
+    __syncthreads();
+    for (int p = tid; p < WINDOW; p += NT) {
+      int id = -1;
+      float ks = 0.f, vs = 0.f;
+      if (((int64_t)(win + p) << pl.page_log2) < t_hi) {
+        id = c.table[(size_t)b * c.max_pages + win + p];
+        if ((unsigned)id >= (unsigned)c.n_pages) id = -1, *s_bad = 1;
+        else ks = c.ks[gi][(size_t)id * c.HKV + h], vs = c.vs[gi][(size_t)id * c.HKV + h];
+      }
+      s_id[p] = id, s_ks[p] = ks, s_vs[p] = vs;
+    }
+    __syncthreads();
+    float most = unit;
+    for (int p = lane; p < WINDOW; p += 64) most = fmaxf(most, s_vs[p]);
+    most = wave_max(most);
+    const float again = most > 0.f ? unit / most : 0.f;
+    if (unit > 0.f && again != 1.f) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i) acc[i] *= again;
+    }
+    unit = most;
+    bad = *s_bad != 0;
+  };
+  uint4 raw[LOADS];
+  uint32_t vf[LOADS];
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int id = i * NT + tid, is_v = id >= 64 * (DH / 16), at = id & (64 * (DH / 16) - 1), r = at / (DH / 16), c16 = at & (DH / 16 - 1);
+      const int key = t + r, pg = (key >> pl.page_log2) - win, pid = key < t_hi ? s_id[pg] : -1;
+      const uint8_t* p = (is_v ? c.v[gi] : c.k[gi]) + (size_t)max(pid, 0) * c.page_bytes + ((size_t)h * c.page + (key & (c.page - 1))) * DH + c16 * 16;
+      raw[i] = pid >= 0 ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
+      const float f = is_v && pid >= 0 && unit > 0.f ? s_vs[pg] / unit * 128.f : 0.f;
+      vf[i] = pack_f16(f, f);
+    }
+  };
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int id = i * NT + tid, is_v = id >= 64 * (DH / 16), at = id & (64 * (DH / 16) - 1), r = at / (DH / 16), c16 = at & (DH / 16 - 1);
+      uint4 lo = wide8<KIND>(raw[i].x, raw[i].y), hi = wide8<KIND>(raw[i].z, raw[i].w);
+      if (is_v) lo = times(lo, vf[i]), hi = times(hi, vf[i]);
+      uint4* p = lds + buf * BUF + is_v * 64 * NCH + r * NCH;
+      p[(2 * c16) ^ swz<DH>(r)] = lo;
+      p[(2 * c16 + 1) ^ swz<DH>(r)] = hi;
+    }
+  };
+
+  if (t_lo < t_hi) {
+    window(t_lo);
+    fetch(t_lo);
+    put(0);
+    __syncthreads();
+  }
+  int buf = 0;
+  for (int t = t_lo; t < t_hi; t += 64) {
+    const bool more = t + 64 < t_hi;
+    const int win_now = win;
+    const bool bad_now = bad;
+    float fk[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) fk[x] = s_ks[min(((t + 16 * x) >> pl.page_log2) - win_now, WINDOW - 1)] * q_scale;
+    unsigned gone = 0;  // 16-key groups that are not there
+    if (bad_now) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) gone |= s_id[min(((t + 16 * x) >> pl.page_log2) - win_now, WINDOW - 1)] < 0 ? 1u << x : 0u;
+    }
+    const bool turn = more && ((t + 64 + 63) >> pl.page_log2) - win >= WINDOW;
+    if (more && !turn) fetch(t + 64);
+    if (t < wave_all) {
+      f32x16 s[2];
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[sub][e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < NK; ++k) s[sub] = mfma32(kr[k][buf * BUF + sub * 32 * NCH], qf[k], s[sub]);
+      }
+      const bool edge = t + 64 > wave_free || gone;
+      float top = m;
+      if (edge) {
+        const int left = min(sees, t_hi) - t - 4 * g;
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int x = 2 * sub + (e >> 3), at = sub * 32 + 8 * (e >> 2) + (e & 3);
+            s[sub][e] = at < left && !(gone >> x & 1) ? s[sub][e] * fk[x] : -__builtin_inff();
+            top = fmaxf(top, s[sub][e]);
+          }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          float big = s[x >> 1][8 * (x & 1)];
+#pragma unroll
+          for (int e = 1; e < 8; ++e) big = fmaxf(big, s[x >> 1][8 * (x & 1) + e]);
+          top = fmaxf(top, big * fk[x]);
+        }
+      }
+      const float2 both = wave_swap32(top);
+      top = fmaxf(both.x, both.y);
+      if (__any(top > m)) {
+        const float keep = fast_exp2(m - top);
+        l *= keep;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) acc[i] *= keep;
+        m = top;
+      }
+      const float off = 15.f - m;
+      float sum = 0.f;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float z = s[x >> 1][8 * (x & 1) + e];
+          p[e] = fast_exp2(edge ? z + off : fmaf(z, fk[x], off));
+          sum += p[e];
+        }
+        const uint4 pf = make_uint4(pack_f16(p[0], p[1]), pack_f16(p[2], p[3]), pack_f16(p[4], p[5]), pack_f16(p[6], p[7]));
+#pragma unroll
+        for (int i = 0; i < NC; ++i) acc[i] = mfma32(read_columns(vc[i], (unsigned)((buf * BUF + 16 * x * NCH) * 16)), pf, acc[i]);
+      }
+      l += sum;
+    }
+    if (turn) {
+      window(t + 64);
+      fetch(t + 64);
+    }
+    if (more) put(buf ^ 1);
+    __syncthreads();
+    buf ^= 1;
+  }
+
+  const float2 both = wave_swap32(l);
+  l = (both.x + both.y) * (1.0f / 32768.f);
+  if (row >= rows) return;
+  const float one = unit * (1.0f / 128.f / 32768.f);
+  const int tok = sq.row0 + j;
+  if (pl.n_split == 1) {
+    const float f = l > 0.f ? one / l : 0.f;
+    bf16_t* dst = a.o[gi] + (size_t)tok * a.ld_o + (size_t)hq * DH;
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<uint2*>(dst + 32 * i + 8 * q + 4 * g) =
+            make_uint2(pack_bf16(acc[i][4 * q] * f, acc[i][4 * q + 1] * f), pack_bf16(acc[i][4 * q + 2] * f, acc[i][4 * q + 3] * f));
+    if (a.lse[gi] && !g) a.lse[gi][(size_t)tok * a.H + hq] = l > 0.f ? m * LN2 + __logf(l) : -__builtin_inff();
+  } else {
+    const size_t part = ((size_t)tok * a.H + hq) * pl.n_split + split;
+    float* po = static_cast<float*>(a.ws[gi]) + part * DH;
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4*>(po + 32 * i + 8 * q + 4 * g) =
+            make_float4(acc[i][4 * q] * one, acc[i][4 * q + 1] * one, acc[i][4 * q + 2] * one, acc[i][4 * q + 3] * one);
+    float2* ml = reinterpret_cast<float2*>(static_cast<float*>(a.ws[gi]) + (size_t)c.n_tok * a.H * pl.n_split * DH);
+    if (!g) ml[part] = make_float2(m, l);
+  }
+}
+
 // The runs' partial sums of one row and head, in ascending order: one wave each.
 template <int DH>
 __global__ __launch_bounds__(256) void cache_attn_join_kernel(const CacheAttnArgs a, const CacheAttnPlan pl) {
@@ -320,14 +599,29 @@ int floor_log2(int v) { return 31 - __builtin_clz((unsigned)v); }
 CacheAttnPlan plan_of(const CacheArgs& c, int H) {
   CacheAttnPlan p{};
   p.page_log2 = floor_log2(c.page);
-  p.n_rt = (int)(((int64_t)c.max_q * (H / c.HKV) + 15) / 16);
-  const int64_t base = (int64_t)c.G * c.B * c.HKV * p.n_rt, want = base >= 4096 ? 1 : (1024 + base - 1) / base;
-  const int64_t most = (c.max_len + 127) / 128;
-  int64_t n = std::min(std::max<int64_t>(want, base >= 4096 ? 1 : (c.max_len + 1023) / 1024), most);
-  if (n < 1) n = 1;
+  const int64_t rows = (int64_t)c.max_q * (H / c.HKV);
+  p.prompt = rows > 64;
+  p.n_rt = (int)((rows + (p.prompt ? 255 : 15)) / (p.prompt ? 256 : 16));
+  const int64_t base = (int64_t)c.G * c.B * c.HKV * p.n_rt;
+  const int64_t unit = p.prompt ? 512 : 128, most = (c.max_len + unit - 1) / unit;
+  int64_t n;
+  if (p.prompt) n = (256 + base - 1) / base;
+  else n = base >= 4096 ? 1 : std::max<int64_t>((1024 + base - 1) / base, (c.max_len + 1023) / 1024);
+  n = std::max<int64_t>(1, std::min(n, most));
   p.chunk = (int)(((c.max_len + n - 1) / n + 127) / 128 * 128);
   p.n_split = (c.max_len + p.chunk - 1) / p.chunk;
   return p;
+}
+
+template <int KIND, int DH>
+hipError_t run_attn(const CacheAttnArgs& a, const CacheAttnPlan& p, dim3 grid, hipStream_t s) {
+  if (p.prompt) hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH, 8>), grid, dim3(512), prompt_lds<DH>(), s, a, p);
+  else hipLaunchKernelGGL((cache_attn_kernel<KIND, DH>), grid, dim3(256), 0, s, a, p);
+  return hipGetLastError();
+}
+template <int KIND, int DH>
+hipError_t prompt_init() {
+  return hipFuncSetAttribute((const void*)cache_prompt_kernel<KIND, DH, 8>, hipFuncAttributeMaxDynamicSharedMemorySize, prompt_lds<DH>());
 }
 
 }  // namespace
@@ -359,6 +653,14 @@ const char* cache_attn_refusal(const CacheAttnArgs& a) {
   return nullptr;
 }
 
+hipError_t cache_attn_init() {
+  hipError_t e;
+  if ((e = prompt_init<CACHE_INT8, 64>()) != hipSuccess) return e;
+  if ((e = prompt_init<CACHE_INT8, 128>()) != hipSuccess) return e;
+  if ((e = prompt_init<CACHE_E4M3, 64>()) != hipSuccess) return e;
+  return prompt_init<CACHE_E4M3, 128>();
+}
+
 hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t s) {
   const CacheArgs& c = a.c;
   CacheAttnPlan p = plan_of(c, a.H);
@@ -366,14 +668,10 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t s) {
   const int64_t bh = (int64_t)c.B * c.HKV, sr = (int64_t)p.n_split * p.n_rt;
   if (bh > 0x7fffffffLL || sr > 65535) return hipErrorInvalidValue;
   const dim3 grid((unsigned)bh, (unsigned)sr, c.G);
-  if (c.kind == CACHE_INT8) {
-    if (c.DH == 64) hipLaunchKernelGGL((cache_attn_kernel<CACHE_INT8, 64>), grid, dim3(256), 0, s, a, p);
-    else hipLaunchKernelGGL((cache_attn_kernel<CACHE_INT8, 128>), grid, dim3(256), 0, s, a, p);
-  } else {
-    if (c.DH == 64) hipLaunchKernelGGL((cache_attn_kernel<CACHE_E4M3, 64>), grid, dim3(256), 0, s, a, p);
-    else hipLaunchKernelGGL((cache_attn_kernel<CACHE_E4M3, 128>), grid, dim3(256), 0, s, a, p);
-  }
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  hipError_t e;
+  if (c.kind == CACHE_INT8) e = c.DH == 64 ? run_attn<CACHE_INT8, 64>(a, p, grid, s) : run_attn<CACHE_INT8, 128>(a, p, grid, s);
+  else e = c.DH == 64 ? run_attn<CACHE_E4M3, 64>(a, p, grid, s) : run_attn<CACHE_E4M3, 128>(a, p, grid, s);
+  if (e != hipSuccess) return e;
   if (p.n_split == 1) return hipSuccess;
   const dim3 join((unsigned)(((int64_t)c.n_tok * a.H + 3) / 4), c.G);
   if (c.DH == 64) hipLaunchKernelGGL((cache_attn_join_kernel<64>), join, dim3(256), 0, s, a, p);

@@ -2221,6 +2221,7 @@ hipError_t kernels_init() {
   hipError_t e;
   if ((e = gemm_init()) != hipSuccess) return e;
   if ((e = ln_init()) != hipSuccess) return e;
+  if ((e = cache_attn_init()) != hipSuccess) return e;
   if ((e = sample_init()) != hipSuccess) return e;
   return attn_init();
 }

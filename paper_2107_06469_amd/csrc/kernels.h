@@ -332,6 +332,7 @@ const char* cache_sizes_refusal(const CacheArgs& c);  // the part that needs no 
 const char* cache_attn_sizes_refusal(const CacheArgs& c, int H);
 const char* cache_attn_refusal(const CacheAttnArgs& a);
 size_t cache_attn_ws_bytes(const CacheArgs& c, int H);
+hipError_t cache_attn_init();
 hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t s);
 
 // ---- drawing tokens (sample.hip) -----------------------------------------------------------------------------------

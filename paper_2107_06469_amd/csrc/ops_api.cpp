@@ -304,6 +304,7 @@ int hydra_op_cache_attention(const hydra_cache_desc* d, int H, int ld_q, int ld_
     a.ws[g] = ws ? ws[g] : nullptr;
   }
   if (const char* why = cache_attn_refusal(a)) return ops_fail(HYDRA_ERR_INVALID_ARG, "hydra_op_cache_attention", why);
+  if (int st = ensure_init()) return st;
   return done(launch_cache_attn(a, static_cast<hipStream_t>(stream)), "hydra_op_cache_attention");
 }
 
