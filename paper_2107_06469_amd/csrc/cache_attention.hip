@@ -291,7 +291,7 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
 // chunk and transposing reads both spread over the banks): codes are widened once for all of a workgroup's rows on their way there.  The
 // next tile's codes are in registers while this one's products run; one barrier a tile.  v_mfma_f32_32x32x16_f16:
 //   S^T[t,i] = K Q^T (lane: query l%32; accumulator rows 8q + 4(l/32) + e),  O^T[d,i] += V^T P^T, P from the accumulators as they are, V^T by transposing
-//   LDS reads.  Values carry 2^7 of their page's scale in units of the window's largest, weights 2^15, so that f16 holds small ones.
+//   LDS reads.  Values carry 2^7 of their page's scale in units of the window's largest, weights 2^7 or more, so that f16 holds small ones.
 // What a window of 512 pages is (id and scales) waits in LDS, too.
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 __device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, f32x16 c) {
@@ -338,6 +338,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
   int* const s_id = reinterpret_cast<int*>(lds + 2 * BUF);
   float* const s_ks = reinterpret_cast<float*>(s_id + WINDOW);
   float* const s_vs = s_ks + WINDOW;
+  uint32_t* const s_vf = reinterpret_cast<uint32_t*>(s_vs);
   int* const s_bad = reinterpret_cast<int*>(s_vs + WINDOW);
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 31, g = lane >> 5;
@@ -422,27 +423,35 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
     }
     unit = most;
     bad = *s_bad != 0;
+    __syncthreads();  // every wave has read the scales
+    for (int p = tid; p < WINDOW; p += NT) {
+      const float f = unit > 0.f ? s_vs[p] / unit * 128.f : 0.f;
+      s_vf[p] = pack_f16(f, f);
+    }
+    __syncthreads();
   };
   uint4 raw[LOADS];
   uint32_t vf[LOADS];
+  // load i of this thread: 16 codes of a tile's keys or (is_v: whole waves) values
+  constexpr int CODES = 64 * (DH / 16);
+  auto is_v = [&](int i) { return (i * NW + wave) * 64 >= CODES; };
   auto fetch = [&](int t) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int id = i * NT + tid, is_v = id >= 64 * (DH / 16), at = id & (64 * (DH / 16) - 1), r = at / (DH / 16), c16 = at & (DH / 16 - 1);
+      const int at = (i * NT + tid) & (CODES - 1), r = at / (DH / 16), c16 = at & (DH / 16 - 1);
       const int key = t + r, pg = (key >> pl.page_log2) - win, pid = key < t_hi ? s_id[pg] : -1;
-      const uint8_t* p = (is_v ? c.v[gi] : c.k[gi]) + (size_t)max(pid, 0) * c.page_bytes + ((size_t)h * c.page + (key & (c.page - 1))) * DH + c16 * 16;
+      const uint8_t* p = (is_v(i) ? c.v[gi] : c.k[gi]) + (size_t)max(pid, 0) * c.page_bytes + ((size_t)h * c.page + (key & (c.page - 1))) * DH + c16 * 16;
       raw[i] = pid >= 0 ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
-      const float f = is_v && pid >= 0 && unit > 0.f ? s_vs[pg] / unit * 128.f : 0.f;
-      vf[i] = pack_f16(f, f);
+      if (is_v(i)) vf[i] = pid >= 0 ? s_vf[pg] : 0u;
     }
   };
-  auto put = [&](int buf) {
+  auto put = [&](uint4* tile) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int id = i * NT + tid, is_v = id >= 64 * (DH / 16), at = id & (64 * (DH / 16) - 1), r = at / (DH / 16), c16 = at & (DH / 16 - 1);
+      const int at = (i * NT + tid) & (CODES - 1), r = at / (DH / 16), c16 = at & (DH / 16 - 1);
       uint4 lo = wide8<KIND>(raw[i].x, raw[i].y), hi = wide8<KIND>(raw[i].z, raw[i].w);
-      if (is_v) lo = times(lo, vf[i]), hi = times(hi, vf[i]);
-      uint4* p = lds + buf * BUF + is_v * 64 * NCH + r * NCH;
+      uint4* p = tile + r * NCH;
+      if (is_v(i)) lo = times(lo, vf[i]), hi = times(hi, vf[i]), p += 64 * NCH;
       p[(2 * c16) ^ swz<DH>(r)] = lo;
       p[(2 * c16 + 1) ^ swz<DH>(r)] = hi;
     }
@@ -451,21 +460,19 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
   if (t_lo < t_hi) {
     window(t_lo);
     fetch(t_lo);
-    put(0);
+    put(lds);
     __syncthreads();
   }
-  int buf = 0;
-  for (int t = t_lo; t < t_hi; t += 64) {
+  auto tile = [&](auto buf_, int t) {
+    constexpr int B = decltype(buf_)::value * BUF;
     const bool more = t + 64 < t_hi;
-    const int win_now = win;
-    const bool bad_now = bad;
     float fk[4];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) fk[x] = s_ks[min(((t + 16 * x) >> pl.page_log2) - win_now, WINDOW - 1)] * q_scale;
+    for (int x = 0; x < 4; ++x) fk[x] = s_ks[min(((t + 16 * x) >> pl.page_log2) - win, WINDOW - 1)] * q_scale;
     unsigned gone = 0;  // 16-key groups that are not there
-    if (bad_now) {
+    if (bad) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) gone |= s_id[min(((t + 16 * x) >> pl.page_log2) - win_now, WINDOW - 1)] < 0 ? 1u << x : 0u;
+      for (int x = 0; x < 4; ++x) gone |= s_id[min(((t + 16 * x) >> pl.page_log2) - win, WINDOW - 1)] < 0 ? 1u << x : 0u;
     }
     const bool turn = more && ((t + 64 + 63) >> pl.page_log2) - win >= WINDOW;
     if (more && !turn) fetch(t + 64);
@@ -476,20 +483,22 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[sub][e] = 0.f;
 #pragma unroll
-        for (int k = 0; k < NK; ++k) s[sub] = mfma32(kr[k][buf * BUF + sub * 32 * NCH], qf[k], s[sub]);
+        for (int k = 0; k < NK; ++k) s[sub] = mfma32(kr[k][B + sub * 32 * NCH], qf[k], s[sub]);
       }
-      const bool edge = t + 64 > wave_free || gone;
-      float top = m;
-      if (edge) {
+      float top = NEG_BIG;
+      if (t + 64 > wave_free || gone) {  // masked, and scaled here already
         const int left = min(sees, t_hi) - t - 4 * g;
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub)
+        for (int x = 0; x < 4; ++x) {
+          const int here = gone >> x & 1 ? 0 : left;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int x = 2 * sub + (e >> 3), at = sub * 32 + 8 * (e >> 2) + (e & 3);
-            s[sub][e] = at < left && !(gone >> x & 1) ? s[sub][e] * fk[x] : -__builtin_inff();
-            top = fmaxf(top, s[sub][e]);
+          for (int e = 0; e < 8; ++e) {
+            const float z = 16 * x + 8 * (e >> 2) + (e & 3) < here ? s[x >> 1][8 * (x & 1) + e] * fk[x] : -__builtin_inff();
+            s[x >> 1][8 * (x & 1) + e] = z;
+            top = fmaxf(top, z);
           }
+          fk[x] = 1.f;
+        }
       } else {
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
@@ -501,43 +510,45 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
       }
       const float2 both = wave_swap32(top);
       top = fmaxf(both.x, both.y);
-      if (__any(top > m)) {
+      // weights are 2^7 of those by the maximum that is held: it may lag by 2^8 (their f16 ends at 2^16) before accumulators are scaled again
+      if (__any(top > m + 8.f)) {
+        top = fmaxf(top, m);
         const float keep = fast_exp2(m - top);
         l *= keep;
 #pragma unroll
         for (int i = 0; i < NC; ++i) acc[i] *= keep;
         m = top;
       }
-      const float off = 15.f - m;
-      float sum = 0.f;
+      const float off = 7.f - m;
+      float sum[4];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         float p[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float z = s[x >> 1][8 * (x & 1) + e];
-          p[e] = fast_exp2(edge ? z + off : fmaf(z, fk[x], off));
-          sum += p[e];
-        }
+        for (int e = 0; e < 8; ++e) p[e] = fast_exp2(fmaf(s[x >> 1][8 * (x & 1) + e], fk[x], off));
+        sum[x] = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
         const uint4 pf = make_uint4(pack_f16(p[0], p[1]), pack_f16(p[2], p[3]), pack_f16(p[4], p[5]), pack_f16(p[6], p[7]));
 #pragma unroll
-        for (int i = 0; i < NC; ++i) acc[i] = mfma32(read_columns(vc[i], (unsigned)((buf * BUF + 16 * x * NCH) * 16)), pf, acc[i]);
+        for (int i = 0; i < NC; ++i) acc[i] = mfma32(read_columns(vc[i], (unsigned)((B + 16 * x * NCH) * 16)), pf, acc[i]);
       }
-      l += sum;
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     }
     if (turn) {
       window(t + 64);
       fetch(t + 64);
     }
-    if (more) put(buf ^ 1);
+    if (more) put(lds + (BUF - B));
     __syncthreads();
-    buf ^= 1;
+  };
+  for (int t = t_lo; t < t_hi; t += 128) {
+    tile(std::integral_constant<int, 0>{}, t);
+    if (t + 64 < t_hi) tile(std::integral_constant<int, 1>{}, t + 64);
   }
 
   const float2 both = wave_swap32(l);
-  l = (both.x + both.y) * (1.0f / 32768.f);
+  l = (both.x + both.y) * (1.0f / 128.f);
   if (row >= rows) return;
-  const float one = unit * (1.0f / 128.f / 32768.f);
+  const float one = unit * (1.0f / 128.f / 128.f);
   const int tok = sq.row0 + j;
   if (pl.n_split == 1) {
     const float f = l > 0.f ? one / l : 0.f;
@@ -601,7 +612,7 @@ CacheAttnPlan plan_of(const CacheArgs& c, int H) {
   p.page_log2 = floor_log2(c.page);
   const int64_t rows = (int64_t)c.max_q * (H / c.HKV);
   p.prompt = rows > 64;
-  p.n_rt = (int)((rows + (p.prompt ? 255 : 15)) / (p.prompt ? 256 : 16));
+  p.n_rt = (int)((rows + (p.prompt ? 127 : 15)) / (p.prompt ? 128 : 16));
   const int64_t base = (int64_t)c.G * c.B * c.HKV * p.n_rt;
   const int64_t unit = p.prompt ? 512 : 128, most = (c.max_len + unit - 1) / unit;
   int64_t n;
@@ -615,13 +626,13 @@ CacheAttnPlan plan_of(const CacheArgs& c, int H) {
 
 template <int KIND, int DH>
 hipError_t run_attn(const CacheAttnArgs& a, const CacheAttnPlan& p, dim3 grid, hipStream_t s) {
-  if (p.prompt) hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH, 8>), grid, dim3(512), prompt_lds<DH>(), s, a, p);
+  if (p.prompt) hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH, 4>), grid, dim3(256), prompt_lds<DH>(), s, a, p);
   else hipLaunchKernelGGL((cache_attn_kernel<KIND, DH>), grid, dim3(256), 0, s, a, p);
   return hipGetLastError();
 }
 template <int KIND, int DH>
 hipError_t prompt_init() {
-  return hipFuncSetAttribute((const void*)cache_prompt_kernel<KIND, DH, 8>, hipFuncAttributeMaxDynamicSharedMemorySize, prompt_lds<DH>());
+  return hipFuncSetAttribute((const void*)cache_prompt_kernel<KIND, DH, 4>, hipFuncAttributeMaxDynamicSharedMemorySize, prompt_lds<DH>());
 }
 
 }  // namespace
