@@ -89,14 +89,23 @@ __device__ __forceinline__ float quarter_sum(float v) {
   return p.x + p.y;
 }
 
+// Codes that one workgroup reads once: past the caches' order of use.
+__device__ __forceinline__ uint4 once16(const uint8_t* p) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)));
+}
+__device__ __forceinline__ uint2 once8(const uint8_t* p) {
+  typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+  return __builtin_bit_cast(uint2, __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p)));
+}
 __device__ __forceinline__ int lane_int(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 __device__ __forceinline__ float lane_float(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
 
 struct CacheAttnPlan {
   int n_split, chunk;  // runs of keys, keys in one (a multiple of 128)
-  int n_rt;            // 16-row tiles of the sequence with the most rows
+  int n_rt;            // 16-row tiles, or 128-row blocks, of the sequence with the most rows
   int page_log2;
-  bool prompt;         // many rows: cache_prompt_kernel, n_rt blocks of 256 rows
+  bool prompt;         // many rows: cache_prompt_kernel
 };
 
 // Four waves share a run of keys, 32 at a time in turn, each with its own maximum, sum and accumulators; they are joined through LDS.
@@ -113,22 +122,63 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
   const CacheSeq sq = cache_seq(c, b);
   const int share = a.H / c.HKV, rows = sq.n * share, first = rt * 16;
   if (first >= rows) return;
+  const int all = a.causal ? max(sq.pos0 + (min(first + 16, rows) - 1) / share + 1, 0) : sq.len;  // keys that the tile's last row sees
+  const int t_lo = split * pl.chunk, t_hi = min(t_lo + pl.chunk, all);
+  // lane i knows page i of a segment of 64 pages; the first one's ids and the queries are asked for together
+  auto page_of = [&](int seg) {
+    int id = -1;
+    if (seg + (lane << pl.page_log2) < t_hi) {
+      id = c.table[(size_t)b * c.max_pages + (seg >> pl.page_log2) + lane];
+      id = (unsigned)id < (unsigned)c.n_pages ? id : -1;
+    }
+    return id;
+  };
+  int id = page_of(t_lo);
   // this lane's row
   const bool have = first + r < rows;
   const int row = have ? first + r : first, j = row / share, hq = h * share + row - j * share;
   const int sees = have ? (a.causal ? max(sq.pos0 + j + 1, 0) : sq.len) : 0;  // keys
-  const int all = a.causal ? max(sq.pos0 + (min(first + 16, rows) - 1) / share + 1, 0) : sq.len;
-  const int t_lo = split * pl.chunk, t_hi = min(t_lo + pl.chunk, all);
+  uint4 q_raw[NK];
+  {
+    const bf16_t* q = a.q[g] + (size_t)(sq.row0 + j) * a.ld_q + (size_t)hq * DH;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) q_raw[k] = *reinterpret_cast<const uint4*>(q + ((k >> 1) * 4 + gq) * 16 + (k & 1) * 8);
+  }
+  // one 32-key tile
+  struct Tile { uint4 k[2][NL]; uint2 v[2][4]; };
+  const int page_mask = c.page - 1;
+  auto fetch = [&](Tile& x, int seg, int t) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int ts = t + 16 * s, pid = max(lane_int(id, (ts - seg) >> pl.page_log2 & 63), 0);
+      const size_t at = (size_t)pid * c.page_bytes + ((size_t)h * c.page + (ts & page_mask)) * DH;
+      const uint8_t* kp = c.k[g] + at + r * DH + gq * 16;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) x.k[s][i] = once16(kp + 64 * i);
+      const uint8_t* vp = c.v[g] + at + gq * 4 * DH + r * W;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (W == 8) x.v[s][e] = once8(vp + e * DH);
+        else x.v[s][e] = make_uint2(__builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(vp + e * DH)), 0u);
+      }
+    }
+  };
+  Tile t0;
+  float ks = 0.f, vs = 0.f;
+  auto scales = [&] {
+    ks = id >= 0 ? c.ks[g][(size_t)id * c.HKV + h] : 0.f, vs = id >= 0 ? c.vs[g][(size_t)id * c.HKV + h] : 0.f;
+  };
+  scales();
+  if (t_lo + wave * 32 < t_hi) fetch(t0, t_lo, t_lo + wave * 32);
 
   uint4 qf[NK];
   float q_scale;
   {
-    const bf16_t* q = a.q[g] + (size_t)(sq.row0 + j) * a.ld_q + (size_t)hq * DH;
     float x[NK][8];
     float most = 0.f;
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
-      const uint4 w = *reinterpret_cast<const uint4*>(q + ((k >> 1) * 4 + gq) * 16 + (k & 1) * 8);
+      const uint4 w = q_raw[k];
       const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -150,16 +200,12 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
 #pragma unroll
   for (int i = 0; i < W; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = NEG_BIG, l = 0.f, unit = 0.f;  // unit: what the accumulators are to be multiplied by
-  const int page_mask = c.page - 1;
   for (int seg = t_lo; seg < t_hi; seg += 64 << pl.page_log2) {
     const int seg_hi = min(t_hi, seg + (64 << pl.page_log2));
-    // lane i knows the segment's page i
-    int id = -1;
-    float ks = 0.f, vs = 0.f;
-    if (seg + (lane << pl.page_log2) < seg_hi) {
-      id = c.table[(size_t)b * c.max_pages + (seg >> pl.page_log2) + lane];
-      if ((unsigned)id >= (unsigned)c.n_pages) id = -1;
-      else ks = c.ks[g][(size_t)id * c.HKV + h], vs = c.vs[g][(size_t)id * c.HKV + h];
+    if (seg > t_lo) {
+      id = page_of(seg);
+      scales();
+      if (seg + wave * 32 < seg_hi) fetch(t0, seg, seg + wave * 32);
     }
     const float unit_now = fmaxf(unit, wave_max(vs));
     const float again = unit_now > 0.f ? unit / unit_now : 0.f;
@@ -167,44 +213,27 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
 #pragma unroll
     for (int i = 0; i < W; ++i) acc[i] *= again;
     unit = unit_now;
-    for (int t = seg + wave * 32; t < seg_hi; t += 128) {
-      uint4 kw[2][NL];
-      uint2 vw[2][4];
-      float kf[2], vf[2];
+    auto use = [&](Tile& x, int t) {
+      float kf[2], vf[2], p[2][4];
       bool ok[2];
+      float top = NEG_BIG;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const int ts = t + 16 * s, pg = (ts - seg) >> pl.page_log2;
-        const int pid = lane_int(id, pg & 63);
-        ok[s] = pid >= 0 && ts < seg_hi;
-        kf[s] = lane_float(ks, pg & 63) * q_scale, vf[s] = lane_float(vs, pg & 63);
-        const size_t at = (size_t)max(pid, 0) * c.page_bytes + ((size_t)h * c.page + (ts & page_mask)) * DH;
-        const uint8_t* kp = c.k[g] + at + r * DH + gq * 16;
-#pragma unroll
-        for (int i = 0; i < NL; ++i) kw[s][i] = *reinterpret_cast<const uint4*>(kp + 64 * i);
-        const uint8_t* vp = c.v[g] + at + gq * 4 * DH + r * W;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (W == 8) vw[s][e] = *reinterpret_cast<const uint2*>(vp + e * DH);
-          else vw[s][e] = make_uint2(*reinterpret_cast<const uint32_t*>(vp + e * DH), 0u);
-        }
+        const int ts = t + 16 * s, pg = (ts - seg) >> pl.page_log2 & 63;
+        ok[s] = lane_int(id, pg) >= 0 && ts < seg_hi;
+        kf[s] = lane_float(ks, pg) * q_scale, vf[s] = lane_float(vs, pg);
         if (KIND == CACHE_E4M3 && (!ok[s] || ts + 16 > seg_hi)) {  // what no token has written may be a NaN
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (!ok[s] || ts + 4 * gq + e >= seg_hi) vw[s][e] = make_uint2(0u, 0u);
+            if (!ok[s] || ts + 4 * gq + e >= seg_hi) x.v[s][e] = make_uint2(0u, 0u);
         }
-      }
-      float p[2][4];
-      float top = m;
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
         f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < NK; ++k) {
-          const uint4& w = kw[s][k >> 1];
+          const uint4& w = x.k[s][k >> 1];
           z = mfma16(k & 1 ? wide8<KIND>(w.z, w.w) : wide8<KIND>(w.x, w.y), qf[k], z);
         }
-        const int left = ok[s] ? min(sees, seg_hi) - (t + 16 * s) - 4 * gq : 0;
+        const int left = ok[s] ? min(sees, seg_hi) - ts - 4 * gq : 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           p[s][e] = e < left ? z[e] * kf[s] : -__builtin_inff();
@@ -212,24 +241,25 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
         }
       }
       top = quarter_max(top);
-      const float keep = fast_exp2(m - top);
-      m = top;
-      float sum = 0.f;
+      if (__any(top > m)) {
+        top = fmaxf(top, m);
+        const float keep = fast_exp2(m - top);
+        m = top, l *= keep;
+#pragma unroll
+        for (int i = 0; i < W; ++i) acc[i] *= keep;
+      }
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          p[s][e] = fast_exp2(p[s][e] - top);
-          sum += p[s][e];
+          p[s][e] = fast_exp2(p[s][e] - m);
+          l += p[s][e];
         }
-      l = l * keep + sum;
-#pragma unroll
-      for (int i = 0; i < W; ++i) acc[i] *= keep;
       const uint4 pf = make_uint4(pack_f16(p[0][0] * vf[0], p[0][1] * vf[0]), pack_f16(p[0][2] * vf[0], p[0][3] * vf[0]),
                                   pack_f16(p[1][0] * vf[1], p[1][1] * vf[1]), pack_f16(p[1][2] * vf[1], p[1][3] * vf[1]));
       auto value = [&](auto c_) {
         constexpr int C = decltype(c_)::value, B = C & 3;
-        auto word = [&](int s, int e) { return C < 4 ? vw[s][e].x : vw[s][e].y; };
+        auto word = [&](int s, int e) { return C < 4 ? x.v[s][e].x : x.v[s][e].y; };
         const uint2 a0 = columns2<KIND, B>(word(0, 0), word(0, 1)), a1 = columns2<KIND, B>(word(0, 2), word(0, 3));
         const uint2 a2 = columns2<KIND, B>(word(1, 0), word(1, 1)), a3 = columns2<KIND, B>(word(1, 2), word(1, 3));
         acc[C] = mfma16(make_uint4(a0.x, a1.x, a2.x, a3.x), pf, acc[C]);
@@ -240,6 +270,16 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
       if constexpr (W == 8) {
         value(std::integral_constant<int, 4>{});
         value(std::integral_constant<int, 6>{});
+      }
+    };
+    int t = seg + wave * 32;
+    Tile t1;  // one tile ahead: what a wave waits for was asked for a tile ago
+    for (; t < seg_hi; t += 256) {
+      if (t + 128 < seg_hi) fetch(t1, seg, t + 128);
+      use(t0, t);
+      if (t + 128 < seg_hi) {
+        if (t + 256 < seg_hi) fetch(t0, seg, t + 256);
+        use(t1, t + 128);
       }
     }
   }
@@ -254,7 +294,7 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
       *reinterpret_cast<f32x4*>(&w_o[wave][r][W * (4 * gq + e) + i]) = v;
     }
   __syncthreads();
-  const int jr = tid >> 4, d0 = (tid & 15) * W;  // joined by 16 threads a row, W columns each
+  const int jr = tid >> 4, at = tid & 15, d0 = at * W;  // joined by 16 threads a row, W columns each
   if (first + jr >= rows) return;
   float mm = NEG_BIG;
 #pragma unroll
@@ -271,18 +311,18 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
   }
   const int tok = sq.row0 + (first + jr) / share, head = h * share + (first + jr) % share;
   if (pl.n_split == 1) {
-    const float f = ll > 0.f ? 1.0f / ll : 0.f;
+    const float f = ll > 0.f ? 1.0f / ll : (ll == 0.f ? 0.f : ll);
     uint32_t* dst = reinterpret_cast<uint32_t*>(a.o[g] + (size_t)tok * a.ld_o + (size_t)head * DH + d0);
 #pragma unroll
     for (int i = 0; i < W; i += 2) dst[i >> 1] = pack_bf16(o[i] * f, o[i + 1] * f);
-    if (a.lse[g] && (tid & 15) == 0) a.lse[g][(size_t)tok * a.H + head] = ll > 0.f ? mm * LN2 + __logf(ll) : -__builtin_inff();
+    if (a.lse[g] && at == 0) a.lse[g][(size_t)tok * a.H + head] = ll > 0.f ? mm * LN2 + __logf(ll) : (ll == 0.f ? -__builtin_inff() : ll);
   } else {
     const size_t part = ((size_t)tok * a.H + head) * pl.n_split + split;
     float* po = static_cast<float*>(a.ws[g]) + part * DH + d0;
 #pragma unroll
     for (int i = 0; i < W; ++i) po[i] = o[i];
     float2* ml = reinterpret_cast<float2*>(static_cast<float*>(a.ws[g]) + (size_t)c.n_tok * a.H * pl.n_split * DH);
-    if ((tid & 15) == 0) ml[part] = make_float2(mm, ll);
+    if (at == 0) ml[part] = make_float2(mm, ll);
   }
 }
 
@@ -551,7 +591,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
   const float one = unit * (1.0f / 128.f / 128.f);
   const int tok = sq.row0 + j;
   if (pl.n_split == 1) {
-    const float f = l > 0.f ? one / l : 0.f;
+    const float f = l > 0.f ? one / l : (l == 0.f ? 0.f : l);
     bf16_t* dst = a.o[gi] + (size_t)tok * a.ld_o + (size_t)hq * DH;
 #pragma unroll
     for (int i = 0; i < NC; ++i)
@@ -559,7 +599,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
       for (int q = 0; q < 4; ++q)
         *reinterpret_cast<uint2*>(dst + 32 * i + 8 * q + 4 * g) =
             make_uint2(pack_bf16(acc[i][4 * q] * f, acc[i][4 * q + 1] * f), pack_bf16(acc[i][4 * q + 2] * f, acc[i][4 * q + 3] * f));
-    if (a.lse[gi] && !g) a.lse[gi][(size_t)tok * a.H + hq] = l > 0.f ? m * LN2 + __logf(l) : -__builtin_inff();
+    if (a.lse[gi] && !g) a.lse[gi][(size_t)tok * a.H + hq] = l > 0.f ? m * LN2 + __logf(l) : (l == 0.f ? -__builtin_inff() : l);
   } else {
     const size_t part = ((size_t)tok * a.H + hq) * pl.n_split + split;
     float* po = static_cast<float*>(a.ws[gi]) + part * DH;
@@ -574,28 +614,38 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
   }
 }
 
-// The runs' partial sums of one row and head, in ascending order: one wave each.
+// The runs' partial sums of one row and head, in ascending order: one wave each.  A lane has the maximum and sum of one run (64 at a time).
 template <int DH>
-__global__ __launch_bounds__(256) void cache_attn_join_kernel(const CacheAttnArgs a, const CacheAttnPlan pl) {
+__global__ __launch_bounds__(64) void cache_attn_join_kernel(const CacheAttnArgs a, const CacheAttnPlan pl) {
   constexpr int E = DH / 64;
-  const int g = blockIdx.y, lane = threadIdx.x & 63;
-  const int64_t n = (int64_t)a.c.n_tok * a.H, i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (i >= n) return;
+  const int g = blockIdx.y, lane = threadIdx.x;
+  const int64_t n = (int64_t)a.c.n_tok * a.H, i = blockIdx.x;
   const int tok = (int)(i / a.H), head = (int)(i - (int64_t)tok * a.H);
   const float* po = static_cast<const float*>(a.ws[g]) + (size_t)i * pl.n_split * DH + lane * E;
   const float2* ml = reinterpret_cast<const float2*>(static_cast<const float*>(a.ws[g]) + (size_t)n * pl.n_split * DH) + (size_t)i * pl.n_split;
   float mm = NEG_BIG;
-  for (int s = 0; s < pl.n_split; ++s) mm = fmaxf(mm, ml[s].x);
+  for (int s0 = 0; s0 < pl.n_split; s0 += 64) mm = fmaxf(mm, s0 + lane < pl.n_split ? ml[s0 + lane].x : NEG_BIG);
+  mm = wave_max(mm);
   float ll = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-  for (int s = 0; s < pl.n_split; ++s) {
-    const float2 v = ml[s];
-    if (v.y > 0.f || v.y != v.y) {
-      const float f = fast_exp2(v.x - mm);
-      ll += v.y * f;
+  for (int s0 = 0; s0 < pl.n_split; s0 += 64) {
+    const float2 v = s0 + lane < pl.n_split ? ml[s0 + lane] : make_float2(NEG_BIG, 0.f);
+    const float w = fast_exp2(v.x - mm);
+    ll += wave_sum(v.y * w);
+    const int cnt = min(64, pl.n_split - s0);
+    for (int s = 0; s < cnt; s += 8) {  // eight loads under way together; past the last run that one again, by 0
+      float x[8][E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] += po[(size_t)s * DH + e] * f;
+      for (int q = 0; q < 8; ++q)
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[q][e] = po[(size_t)(s0 + min(s + q, cnt - 1)) * DH + e];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const float f = s + q < cnt ? lane_float(w, s + q) : 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] += x[q][e] * f;
+      }
     }
   }
   const float f = ll > 0.f ? 1.0f / ll : (ll == 0.f ? 0.f : ll);
@@ -610,17 +660,15 @@ int floor_log2(int v) { return 31 - __builtin_clz((unsigned)v); }
 CacheAttnPlan plan_of(const CacheArgs& c, int H) {
   CacheAttnPlan p{};
   p.page_log2 = floor_log2(c.page);
-  const int64_t rows = (int64_t)c.max_q * (H / c.HKV);
+  const int64_t rows = (int64_t)c.max_q * (H / c.HKV), len = c.max_len;
   p.prompt = rows > 64;
   p.n_rt = (int)((rows + (p.prompt ? 127 : 15)) / (p.prompt ? 128 : 16));
   const int64_t base = (int64_t)c.G * c.B * c.HKV * p.n_rt;
-  const int64_t unit = p.prompt ? 512 : 128, most = (c.max_len + unit - 1) / unit;
   int64_t n;
-  if (p.prompt) n = (256 + base - 1) / base;
-  else n = base >= 4096 ? 1 : std::max<int64_t>((1024 + base - 1) / base, (c.max_len + 1023) / 1024);
-  n = std::max<int64_t>(1, std::min(n, most));
-  p.chunk = (int)(((c.max_len + n - 1) / n + 127) / 128 * 128);
-  p.n_split = (c.max_len + p.chunk - 1) / p.chunk;
+  if (p.prompt) n = std::min((256 + base - 1) / base, (len + 511) / 512);
+  else n = std::min(std::max((512 + base - 1) / base, (len + 4095) / 4096), (len + 127) / 128);
+  p.chunk = (int)(((len + n - 1) / n + 127) / 128 * 128);
+  p.n_split = (int)((len + p.chunk - 1) / p.chunk);
   return p;
 }
 
@@ -631,7 +679,7 @@ hipError_t run_attn(const CacheAttnArgs& a, const CacheAttnPlan& p, dim3 grid, h
   return hipGetLastError();
 }
 template <int KIND, int DH>
-hipError_t prompt_init() {
+hipError_t attn_init_kind() {
   return hipFuncSetAttribute((const void*)cache_prompt_kernel<KIND, DH, 4>, hipFuncAttributeMaxDynamicSharedMemorySize, prompt_lds<DH>());
 }
 
@@ -666,10 +714,10 @@ const char* cache_attn_refusal(const CacheAttnArgs& a) {
 
 hipError_t cache_attn_init() {
   hipError_t e;
-  if ((e = prompt_init<CACHE_INT8, 64>()) != hipSuccess) return e;
-  if ((e = prompt_init<CACHE_INT8, 128>()) != hipSuccess) return e;
-  if ((e = prompt_init<CACHE_E4M3, 64>()) != hipSuccess) return e;
-  return prompt_init<CACHE_E4M3, 128>();
+  if ((e = attn_init_kind<CACHE_INT8, 64>()) != hipSuccess) return e;
+  if ((e = attn_init_kind<CACHE_INT8, 128>()) != hipSuccess) return e;
+  if ((e = attn_init_kind<CACHE_E4M3, 64>()) != hipSuccess) return e;
+  return attn_init_kind<CACHE_E4M3, 128>();
 }
 
 hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t s) {
@@ -684,9 +732,10 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t s) {
   else e = c.DH == 64 ? run_attn<CACHE_E4M3, 64>(a, p, grid, s) : run_attn<CACHE_E4M3, 128>(a, p, grid, s);
   if (e != hipSuccess) return e;
   if (p.n_split == 1) return hipSuccess;
-  const dim3 join((unsigned)(((int64_t)c.n_tok * a.H + 3) / 4), c.G);
-  if (c.DH == 64) hipLaunchKernelGGL((cache_attn_join_kernel<64>), join, dim3(256), 0, s, a, p);
-  else hipLaunchKernelGGL((cache_attn_join_kernel<128>), join, dim3(256), 0, s, a, p);
+  if ((int64_t)c.n_tok * a.H > 0x7fffffffLL) return hipErrorInvalidValue;
+  const dim3 join((unsigned)((int64_t)c.n_tok * a.H), c.G);
+  if (c.DH == 64) hipLaunchKernelGGL((cache_attn_join_kernel<64>), join, dim3(64), 0, s, a, p);
+  else hipLaunchKernelGGL((cache_attn_join_kernel<128>), join, dim3(64), 0, s, a, p);
   return hipGetLastError();
 }
 
