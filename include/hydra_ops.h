@@ -184,8 +184,14 @@ typedef struct {
  * round(x * (1 / scale)), to nearest even.  Infinities become the largest code and do not count for a scale, NaN becomes 0.  Slots past a
  * sequence's last token keep what they have.  A page may belong to one sequence of the call only, unless nothing is appended to it.
  * Tokens at positions below 0 (lens[b] less than the tokens of the call) are dropped. */
-int hydra_op_cache_append(const hydra_cache_desc* cache, int H, int ld_qkv, int ld_q, int rot, int rot_dim, const float* cos_sin,
-                          const void* const* qkv, void* const* q, void* stream);
+typedef struct {
+  hydra_cache_desc cache;
+  int H, ld_qkv, ld_q, rot, rot_dim;
+  const float* cos_sin;
+  const void* const* qkv;
+  void* const* q;
+} hydra_cache_append_desc;
+int hydra_op_cache_append(const hydra_cache_append_desc* d, void* stream);
 
 /* o_i = sum_t softmax_t(scale * q_i . k_t) v_t over the tokens t that the cache holds of the row's sequence, with causal those up to the
  * row's own position.  q_g [n_tok, ld_q] and o_g [n_tok, ld_o] bf16, H heads of DH columns; query head i reads key/value head i / (H/HKV).
@@ -195,8 +201,17 @@ int hydra_op_cache_append(const hydra_cache_desc* cache, int H, int ld_qkv, int 
  * ws_g: device scratch of hydra_op_cache_attention_ws_bytes bytes, 16-byte aligned, so that a sequence's tokens can be split over
  * workgroups whose results are joined in ascending order; it need not be initialised.  Without it (or with too little) nothing is split.
  * The size and the split depend on the descriptor's sizes and H alone. */
-int hydra_op_cache_attention(const hydra_cache_desc* cache, int H, int ld_q, int ld_o, int causal, float scale, const void* const* q,
-                             void* const* o, float* const* lse, void* const* ws, size_t ws_bytes, void* stream);
+typedef struct {
+  hydra_cache_desc cache;
+  int H, ld_q, ld_o, causal;
+  float scale;
+  const void* const* q;
+  void* const* o;
+  float* const* lse;
+  void* const* ws;
+  size_t ws_bytes;
+} hydra_cache_attention_desc;
+int hydra_op_cache_attention(const hydra_cache_attention_desc* d, void* stream);
 size_t hydra_op_cache_attention_ws_bytes(const hydra_cache_desc* cache, int H);
 
 /* One token per row of logits_g [rows, ldz] (fp32 or bf16, V columns, 262144 at most), drawn from given uniforms u_g [rows, ldu] in [0, 1), one per token.

@@ -28,7 +28,7 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_BIG = -1.0e30f;
-constexpr float P_ONE = 32768.f;  // a weight of 1 in f16
+constexpr float P_LOG2 = 15.f, P_ONE = 32768.f;  // a weight of 1 in f16
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
@@ -44,35 +44,35 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
 __device__ __forceinline__ f32x4 mfma16(const uint4& a, const uint4& b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-// int8 codes in the low bytes of two halves -> f16: with the sign bit turned over a code c is 128 + c, which under the exponent of 1024 is 1152 + c
-__device__ __forceinline__ uint32_t int8_halves(uint32_t w) {
-  const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
-  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, w ^ 0x64806480u) - off);
-}
+// An int8 code c with its sign bit turned over is u = 128 + c.  In a half by itself u is a (subnormal) f16 number, u 2^-24, which the matrix
+// cores take as any other.  What the 128 add to a score is known beforehand: its accumulator begins there.  From values they are taken off at once (c 2^-24 is
+// exact, too): taken off a sum they would leave 2^-17 of the largest code in columns that are small.
+constexpr float U_ONE = 16777216.f;  // 2^24
+template <int KIND>
+__device__ __forceinline__ uint32_t turned(uint32_t w) { return KIND == CACHE_INT8 ? w ^ 0x80808080u : w; }
 template <bool HI>
 __device__ __forceinline__ uint32_t e4m3_halves(uint32_t w) {
   return __builtin_bit_cast(uint32_t, (f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HI));
 }
-// the low (high) two codes of a word as f16
-template <int KIND, bool HI>
-__device__ __forceinline__ uint32_t halves(uint32_t w) {
-  if (KIND == CACHE_E4M3) return e4m3_halves<HI>(w);
-  return int8_halves(__builtin_amdgcn_perm(0, w, HI ? 0x0c030c02u : 0x0c010c00u));
-}
-// eight codes in a row
+// eight codes in a row: their values, or of int8 u 2^-24
 template <int KIND>
 __device__ __forceinline__ uint4 wide8(uint32_t lo, uint32_t hi) {
-  return make_uint4(halves<KIND, false>(lo), halves<KIND, true>(lo), halves<KIND, false>(hi), halves<KIND, true>(hi));
+  if (KIND == CACHE_E4M3) return make_uint4(e4m3_halves<false>(lo), e4m3_halves<true>(lo), e4m3_halves<false>(hi), e4m3_halves<true>(hi));
+  lo = turned<KIND>(lo), hi = turned<KIND>(hi);
+  return make_uint4(__builtin_amdgcn_perm(0, lo, 0x0c010c00u), __builtin_amdgcn_perm(0, lo, 0x0c030c02u), __builtin_amdgcn_perm(0, hi, 0x0c010c00u),
+                    __builtin_amdgcn_perm(0, hi, 0x0c030c02u));
 }
-// bytes C and C + 1 (C even) of two keys' words -> {key 0, key 1} of column C and of column C + 1
+// bytes C and C + 1 (C even) of two keys' (turned) words -> {key 0, key 1} of column C and of column C + 1, of int8 times 2^-24
 template <int KIND, int C>
 __device__ __forceinline__ uint2 columns2(uint32_t k0, uint32_t k1) {
   if (KIND == CACHE_E4M3) {
     const uint32_t w = __builtin_amdgcn_perm(k1, k0, (unsigned)C | (4u + C) << 8 | (1u + C) << 16 | (5u + C) << 24);
     return make_uint2(e4m3_halves<false>(w), e4m3_halves<true>(w));
   }
-  return make_uint2(int8_halves(__builtin_amdgcn_perm(k1, k0, 0x0c000c00u | C | (4u + C) << 16)),
-                    int8_halves(__builtin_amdgcn_perm(k1, k0, 0x0c000c00u | (C + 1) | (5u + C) << 16)));
+  auto code = [&](uint32_t sel) {
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(k1, k0, sel)) + __builtin_bit_cast(f16x2, 0x80808080u));  // - 128 2^-24
+  };
+  return make_uint2(code(0x0c000c00u | C | (4u + C) << 16), code(0x0c000c00u | (C + 1) | (5u + C) << 16));
 }
 
 // max over the four lanes that share l%16
@@ -89,6 +89,19 @@ __device__ __forceinline__ float quarter_sum(float v) {
   return p.x + p.y;
 }
 
+__device__ __forceinline__ float sum8(const uint4& v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f16x2 h = __builtin_bit_cast(f16x2, w[i]);
+    s += (float)h.x + (float)h.y;
+  }
+  return s;
+}
+__device__ __forceinline__ uint32_t times2(uint32_t v, uint32_t f) {
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v) * __builtin_bit_cast(f16x2, f));
+}
 // Codes that one workgroup reads once: past the caches' order of use.
 __device__ __forceinline__ uint4 once16(const uint8_t* p) {
   typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
@@ -138,6 +151,7 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
   const bool have = first + r < rows;
   const int row = have ? first + r : first, j = row / share, hq = h * share + row - j * share;
   const int sees = have ? (a.causal ? max(sq.pos0 + j + 1, 0) : sq.len) : 0;  // keys
+  const int free = min(t_hi, a.causal ? sq.pos0 + first / share + 1 : sq.len);  // keys that every row of the tile sees
   uint4 q_raw[NK];
   {
     const bf16_t* q = a.q[g] + (size_t)(sq.row0 + j) * a.ld_q + (size_t)hq * DH;
@@ -154,7 +168,7 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
       const size_t at = (size_t)pid * c.page_bytes + ((size_t)h * c.page + (ts & page_mask)) * DH;
       const uint8_t* kp = c.k[g] + at + r * DH + gq * 16;
 #pragma unroll
-      for (int i = 0; i < NL; ++i) x.k[s][i] = once16(kp + 64 * i);
+      for (int i = 0; i < NL; ++i) x.k[s][i] = *reinterpret_cast<const uint4*>(kp + 64 * i);  // (a row of 128 bytes by two loads: through the cache)
       const uint8_t* vp = c.v[g] + at + gq * 4 * DH + r * W;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -195,6 +209,14 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
       qf[k] = make_uint4(pack_f16(x[k][0] * f, x[k][1] * f), pack_f16(x[k][2] * f, x[k][3] * f), pack_f16(x[k][4] * f, x[k][5] * f),
                          pack_f16(x[k][6] * f, x[k][7] * f));
   }
+  float begin = 0.f;  // of a score's accumulator
+  if (KIND == CACHE_INT8) {
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) sum += sum8(qf[k]);
+    begin = quarter_sum(sum) * (-128.f / U_ONE);
+    q_scale *= U_ONE;
+  }
 
   f32x4 acc[W];
 #pragma unroll
@@ -209,36 +231,49 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
     }
     const float unit_now = fmaxf(unit, wave_max(vs));
     const float again = unit_now > 0.f ? unit / unit_now : 0.f;
-    vs = unit_now > 0.f ? vs / unit_now * P_ONE : 0.f;
+    const uint32_t vr = pack_f16(unit_now > 0.f ? vs / unit_now : 0.f, unit_now > 0.f ? vs / unit_now : 0.f);
+    if (seg > t_lo) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) acc[i] *= again;
+      for (int i = 0; i < W; ++i) acc[i] *= again;
+    }
     unit = unit_now;
     auto use = [&](Tile& x, int t) {
-      float kf[2], vf[2], p[2][4];
+      float kf[2], p[2][4];
+      uint32_t vf[2];
       bool ok[2];
-      float top = NEG_BIG;
+      f32x4 z[2];
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const int ts = t + 16 * s, pg = (ts - seg) >> pl.page_log2 & 63;
         ok[s] = lane_int(id, pg) >= 0 && ts < seg_hi;
-        kf[s] = lane_float(ks, pg) * q_scale, vf[s] = lane_float(vs, pg);
+        kf[s] = lane_float(ks, pg) * q_scale, vf[s] = (uint32_t)lane_int((int)vr, pg);
         if (KIND == CACHE_E4M3 && (!ok[s] || ts + 16 > seg_hi)) {  // what no token has written may be a NaN
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (!ok[s] || ts + 4 * gq + e >= seg_hi) x.v[s][e] = make_uint2(0u, 0u);
         }
-        f32x4 z = {0.f, 0.f, 0.f, 0.f};
+        z[s] = f32x4{begin, begin, begin, begin};
 #pragma unroll
         for (int k = 0; k < NK; ++k) {
           const uint4& w = x.k[s][k >> 1];
-          z = mfma16(k & 1 ? wide8<KIND>(w.z, w.w) : wide8<KIND>(w.x, w.y), qf[k], z);
+          z[s] = mfma16(k & 1 ? wide8<KIND>(w.z, w.w) : wide8<KIND>(w.x, w.y), qf[k], z[s]);
         }
-        const int left = ok[s] ? min(sees, seg_hi) - ts - 4 * gq : 0;
+      }
+      float top;
+      if (t + 32 > free || !ok[0] || !ok[1]) {  // masked, and scaled here already
+        top = NEG_BIG;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[s][e] = e < left ? z[e] * kf[s] : -__builtin_inff();
-          top = fmaxf(top, p[s][e]);
+        for (int s = 0; s < 2; ++s) {
+          const int left = ok[s] ? min(sees, seg_hi) - (t + 16 * s) - 4 * gq : 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            z[s][e] = e < left ? z[s][e] * kf[s] : -__builtin_inff();
+            top = fmaxf(top, z[s][e]);
+          }
+          kf[s] = 1.f;
         }
+      } else {
+        top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])) * kf[0], fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])) * kf[1]);
       }
       top = quarter_max(top);
       if (__any(top > m)) {
@@ -248,15 +283,21 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
 #pragma unroll
         for (int i = 0; i < W; ++i) acc[i] *= keep;
       }
+      const float off = P_LOG2 - m;
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+      for (int s = 0; s < 2; ++s) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[s][e] = fast_exp2(p[s][e] - m);
-          l += p[s][e];
-        }
-      const uint4 pf = make_uint4(pack_f16(p[0][0] * vf[0], p[0][1] * vf[0]), pack_f16(p[0][2] * vf[0], p[0][3] * vf[0]),
-                                  pack_f16(p[1][0] * vf[1], p[1][1] * vf[1]), pack_f16(p[1][2] * vf[1], p[1][3] * vf[1]));
+        for (int e = 0; e < 4; ++e) p[s][e] = fast_exp2(fmaf(z[s][e], kf[s], off));
+        l += (p[s][0] + p[s][1]) + (p[s][2] + p[s][3]);
+      }
+      const uint4 pf = make_uint4(times2(pack_f16(p[0][0], p[0][1]), vf[0]), times2(pack_f16(p[0][2], p[0][3]), vf[0]),
+                                  times2(pack_f16(p[1][0], p[1][1]), vf[1]), times2(pack_f16(p[1][2], p[1][3]), vf[1]));
+      if (KIND == CACHE_INT8) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x.v[s][e] = make_uint2(turned<KIND>(x.v[s][e].x), W == 8 ? turned<KIND>(x.v[s][e].y) : 0u);
+      }
       auto value = [&](auto c_) {
         constexpr int C = decltype(c_)::value, B = C & 3;
         auto word = [&](int s, int e) { return C < 4 ? x.v[s][e].x : x.v[s][e].y; };
@@ -283,15 +324,16 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
       }
     }
   }
-  l = quarter_sum(l);
+  l = quarter_sum(l) * (1.0f / P_ONE);
+  const float one = unit * (KIND == CACHE_INT8 ? U_ONE / P_ONE : 1.0f / P_ONE);
 
   if (gq == 0) w_ml[wave][r] = make_float2(m, l);
 #pragma unroll
   for (int e = 0; e < 4; ++e)
 #pragma unroll
     for (int i = 0; i < W; i += 4) {
-      const f32x4 v = f32x4{acc[i][e], acc[i + 1][e], acc[i + 2][e], acc[i + 3][e]} * (unit * (1.0f / P_ONE));
-      *reinterpret_cast<f32x4*>(&w_o[wave][r][W * (4 * gq + e) + i]) = v;
+      const f32x4 v = f32x4{acc[i][e], acc[i + 1][e], acc[i + 2][e], acc[i + 3][e]};
+      *reinterpret_cast<f32x4*>(&w_o[wave][r][W * (4 * gq + e) + i]) = v * one;
     }
   __syncthreads();
   const int jr = tid >> 4, at = tid & 15, d0 = at * W;  // joined by 16 threads a row, W columns each
@@ -359,9 +401,14 @@ __device__ __forceinline__ uint4 read_columns(const ColumnsAt& c, unsigned off) 
   const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(c.a1 + off)));
   return make_uint4(lo.x, lo.y, hi.x, hi.y);
 }
-__device__ __forceinline__ uint4 times(const uint4& v, uint32_t f) {
-  const f16x2 m = __builtin_bit_cast(f16x2, f);
-  auto one = [&](uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, w) * m); };
+// What wide8 gives as values times f: u as 1024 + u (the exponent goes beside it), less 1152
+template <int KIND>
+__device__ __forceinline__ uint4 value_of(const uint4& v, uint32_t f) {
+  const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
+  auto one = [&](uint32_t w) {
+    if (KIND == CACHE_INT8) w = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, w | 0x64006400u) - off);
+    return times2(w, f);
+  };
   return make_uint4(one(v.x), one(v.y), one(v.z), one(v.w));
 }
 constexpr int WINDOW = 512;
@@ -421,6 +468,15 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
     }
   }
 
+  float begin = 0.f;  // of a score's accumulator
+  if (KIND == CACHE_INT8) {
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) sum += sum8(qf[k]);
+    const float2 both = wave_swap32(sum);
+    begin = (both.x + both.y) * (-128.f / U_ONE);
+    q_scale *= U_ONE;
+  }
   const uint4* kr[NK];
   ColumnsAt vc[NC];
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char*)reinterpret_cast<const char*>(lds);
@@ -491,7 +547,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
       const int at = (i * NT + tid) & (CODES - 1), r = at / (DH / 16), c16 = at & (DH / 16 - 1);
       uint4 lo = wide8<KIND>(raw[i].x, raw[i].y), hi = wide8<KIND>(raw[i].z, raw[i].w);
       uint4* p = tile + r * NCH;
-      if (is_v(i)) lo = times(lo, vf[i]), hi = times(hi, vf[i]), p += 64 * NCH;
+      if (is_v(i)) lo = value_of<KIND>(lo, vf[i]), hi = value_of<KIND>(hi, vf[i]), p += 64 * NCH;
       p[(2 * c16) ^ swz<DH>(r)] = lo;
       p[(2 * c16 + 1) ^ swz<DH>(r)] = hi;
     }
@@ -521,7 +577,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[sub][e] = 0.f;
+        for (int e = 0; e < 16; ++e) s[sub][e] = begin;
 #pragma unroll
         for (int k = 0; k < NK; ++k) s[sub] = mfma32(kr[k][B + sub * 32 * NCH], qf[k], s[sub]);
       }
@@ -666,7 +722,7 @@ CacheAttnPlan plan_of(const CacheArgs& c, int H) {
   const int64_t base = (int64_t)c.G * c.B * c.HKV * p.n_rt;
   int64_t n;
   if (p.prompt) n = std::min((256 + base - 1) / base, (len + 511) / 512);
-  else n = std::min(std::max((512 + base - 1) / base, (len + 4095) / 4096), (len + 127) / 128);
+  else n = len <= 640 ? 1 : std::min(std::max((512 + base - 1) / base, (len + 4095) / 4096), (len + 127) / 128);
   p.chunk = (int)(((len + n - 1) / n + 127) / 128 * 128);
   p.n_split = (int)((len + p.chunk - 1) / p.chunk);
   return p;

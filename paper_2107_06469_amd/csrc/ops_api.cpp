@@ -271,15 +271,14 @@ static bool cache_tables(const hydra_cache_desc* d) {
 
 extern "C" {
 
-int hydra_op_cache_append(const hydra_cache_desc* d, int H, int ld_qkv, int ld_q, int rot, int rot_dim, const float* cos_sin,
-                          const void* const* qkv, void* const* q, void* stream) {
-  if (!cache_tables(d) || !qkv) return bad("hydra_op_cache_append: NULL table or G out of range");
+int hydra_op_cache_append(const hydra_cache_append_desc* d, void* stream) {
+  if (!d || !cache_tables(&d->cache) || !d->qkv) return bad("hydra_op_cache_append: NULL table or G out of range");
   AppendArgs a{};
-  a.c = cache_args(d);
-  a.H = H; a.ld_qkv = ld_qkv; a.ld_q = ld_q; a.rot = rot; a.rot_dim = rot_dim; a.cs = cos_sin; a.has_q = q != nullptr;
-  for (int g = 0; g < d->G; ++g) {
-    a.qkv[g] = static_cast<const bf16_t*>(qkv[g]);
-    a.q[g] = q ? static_cast<bf16_t*>(q[g]) : nullptr;
+  a.c = cache_args(&d->cache);
+  a.H = d->H; a.ld_qkv = d->ld_qkv; a.ld_q = d->ld_q; a.rot = d->rot; a.rot_dim = d->rot_dim; a.cs = d->cos_sin; a.has_q = d->q != nullptr;
+  for (int g = 0; g < a.c.G; ++g) {
+    a.qkv[g] = static_cast<const bf16_t*>(d->qkv[g]);
+    a.q[g] = d->q ? static_cast<bf16_t*>(d->q[g]) : nullptr;
   }
   if (const char* why = append_refusal(a)) return ops_fail(HYDRA_ERR_INVALID_ARG, "hydra_op_cache_append", why);
   return done(launch_append(a, static_cast<hipStream_t>(stream)), "hydra_op_cache_append");
@@ -291,17 +290,16 @@ size_t hydra_op_cache_attention_ws_bytes(const hydra_cache_desc* d, int H) {
   return cache_attn_sizes_refusal(c, H) ? 0 : cache_attn_ws_bytes(c, H);
 }
 
-int hydra_op_cache_attention(const hydra_cache_desc* d, int H, int ld_q, int ld_o, int causal, float scale, const void* const* q,
-                             void* const* o, float* const* lse, void* const* ws, size_t ws_bytes, void* stream) {
-  if (!cache_tables(d) || !q || !o) return bad("hydra_op_cache_attention: NULL table or G out of range");
+int hydra_op_cache_attention(const hydra_cache_attention_desc* d, void* stream) {
+  if (!d || !cache_tables(&d->cache) || !d->q || !d->o) return bad("hydra_op_cache_attention: NULL table or G out of range");
   CacheAttnArgs a{};
-  a.c = cache_args(d);
-  a.H = H; a.ld_q = ld_q; a.ld_o = ld_o; a.causal = causal; a.scale = scale; a.ws_bytes = ws ? ws_bytes : 0;
-  for (int g = 0; g < d->G; ++g) {
-    a.q[g] = static_cast<const bf16_t*>(q[g]);
-    a.o[g] = static_cast<bf16_t*>(o[g]);
-    a.lse[g] = lse ? lse[g] : nullptr;
-    a.ws[g] = ws ? ws[g] : nullptr;
+  a.c = cache_args(&d->cache);
+  a.H = d->H; a.ld_q = d->ld_q; a.ld_o = d->ld_o; a.causal = d->causal; a.scale = d->scale; a.ws_bytes = d->ws ? d->ws_bytes : 0;
+  for (int g = 0; g < a.c.G; ++g) {
+    a.q[g] = static_cast<const bf16_t*>(d->q[g]);
+    a.o[g] = static_cast<bf16_t*>(d->o[g]);
+    a.lse[g] = d->lse ? d->lse[g] : nullptr;
+    a.ws[g] = d->ws ? d->ws[g] : nullptr;
   }
   if (const char* why = cache_attn_refusal(a)) return ops_fail(HYDRA_ERR_INVALID_ARG, "hydra_op_cache_attention", why);
   if (int st = ensure_init()) return st;

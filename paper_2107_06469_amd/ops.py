@@ -60,8 +60,8 @@ def _L():
         L.hydra_op_attention_bwd.argtypes = [C.c_int] * 7 + [C.c_float, C.c_int] + [pp] * 6 + [vp]
         L.hydra_op_embed_fwd.argtypes = [C.c_int] * 6 + [vp, pp, pp, pp, vp]
         L.hydra_op_embed_bwd.argtypes = [C.c_int] * 8 + [vp, vp, pp, pp, pp, vp]
-        L.hydra_op_cache_append.argtypes = [vp] + [C.c_int] * 5 + [vp, pp, pp, vp]
-        L.hydra_op_cache_attention.argtypes = [vp] + [C.c_int] * 4 + [C.c_float] + [pp] * 4 + [C.c_size_t, vp]
+        L.hydra_op_cache_append.argtypes = [vp, vp]
+        L.hydra_op_cache_attention.argtypes = [vp, vp]
         L.hydra_op_cache_attention_ws_bytes.argtypes = [vp, C.c_int]
         L.hydra_op_cache_attention_ws_bytes.restype = C.c_size_t
         L.hydra_op_sample.argtypes = [C.c_int] * 6 + [pp, pp, vp, vp, vp, vp, pp, pp, vp]
@@ -240,35 +240,37 @@ class Cache:
         self.HKV, self.page, self.DH, self.G = hkv, page, dh, len(k)
         self._head = (kind, self.B, hkv, dh, page, n_pages, self.max_pages, self.G)
         self._stride = stride if n_pages > 1 else 0
+        self._table = page_table.data_ptr()
         self._keep, *self._at = _tabs(k, v, k_scale, v_scale)
 
-    def desc(self, lens=None, q_ptr=None, n_tok=None, max_q=1, max_len=None):
-        """The packed hydra_cache_desc of a call."""
-        return _cache_desc(*self._head, self.B if n_tok is None else n_tok, max_q, self.max_pages * self.page if max_len is None else max_len,
-                           self._stride, self.page_table.data_ptr(), 0 if lens is None else lens.data_ptr(),
-                           0 if q_ptr is None else q_ptr.data_ptr(), *self._at)
+    def fields(self, lens=None, q_ptr=None, n_tok=None, max_q=1, max_len=None):
+        """The fields of a call's hydra_cache_desc."""
+        return (*self._head, self.B if n_tok is None else n_tok, max_q, self.max_pages * self.page if max_len is None else max_len, self._stride,
+                self._table, 0 if lens is None else lens.data_ptr(), 0 if q_ptr is None else q_ptr.data_ptr(), *self._at)
 
 
-_cache_desc = struct.Struct("11iN7P").pack      # the fields of hydra_cache_desc
+# hydra_cache_desc, and with what an operator adds to it
+_cache_desc, _append_desc, _attention_desc = (struct.Struct("11iN7P" + more).pack for more in ("", "5i3P", "4if4PN"))
 
 
 def hydra_op_cache_append(cache, lens, H, ld_qkv, ld_q, qkv, q=None, *, rot=ROT_NONE, rot_dim=0, cos_sin=None, q_ptr=None, n_tok=None, max_q=1,
                           max_len=None):
     """q=None leaves the queries alone; max_len=None: as many tokens as the page table has room for."""
-    keep, *at = _tabs(qkv, q)
-    _check(_L().hydra_op_cache_append(cache.desc(lens, q_ptr, n_tok, max_q, max_len), H, ld_qkv, ld_q, rot, rot_dim,
-                                      None if cos_sin is None else cos_sin.data_ptr(), *at, _stream()))
+    keep, tqkv, tq = _tabs(qkv, q)
+    d = _append_desc(*cache.fields(lens, q_ptr, n_tok, max_q, max_len), H, ld_qkv, ld_q, rot, rot_dim, 0 if cos_sin is None else cos_sin.data_ptr(), tqkv,
+                     tq or 0)
+    _check(_L().hydra_op_cache_append(d, _stream()))
 
 
 def hydra_op_cache_attention_ws_bytes(cache, H, *, n_tok=None, max_q=1, max_len=None) -> int:
-    return int(_L().hydra_op_cache_attention_ws_bytes(cache.desc(n_tok=n_tok, max_q=max_q, max_len=max_len), H))
+    return int(_L().hydra_op_cache_attention_ws_bytes(_cache_desc(*cache.fields(n_tok=n_tok, max_q=max_q, max_len=max_len)), H))
 
 
 def hydra_op_cache_attention(cache, lens, H, ld_q, ld_o, causal, scale, q, o, lse=None, *, ws=None, q_ptr=None, n_tok=None, max_q=1, max_len=None):
     """ws: optional per-model scratch tensors (uint8, hydra_op_cache_attention_ws_bytes bytes) that allow splitting a sequence's tokens."""
-    keep, *at = _tabs(q, o, lse, ws)
-    _check(_L().hydra_op_cache_attention(cache.desc(lens, q_ptr, n_tok, max_q, max_len), H, ld_q, ld_o, int(causal), scale, *at, _nbytes(ws),
-                                         _stream()))
+    keep, tq, to, tl, tw = _tabs(q, o, lse, ws)
+    d = _attention_desc(*cache.fields(lens, q_ptr, n_tok, max_q, max_len), H, ld_q, ld_o, causal, scale, tq, to, tl or 0, tw or 0, _nbytes(ws))
+    _check(_L().hydra_op_cache_attention(d, _stream()))
 
 
 def hydra_op_sample(dtype, rows, V, ldz, ldu, logits, u, temperature, top_k, top_p, min_p, token, logprob=None):

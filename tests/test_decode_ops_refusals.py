@@ -13,8 +13,7 @@ def cache(G=1, table=True, **kw):
     d = dict(kind=0, B=3, HKV=2, DH=128, page=64, n_pages=10, max_pages=4, G=G, n_tok=3, max_q=1, max_len=256, page_bytes=0, page_table=A, lens=A, q_ptr=0)
     d.update(kw)
     tabs = [(C.c_void_p * 16)(*[d.pop(n, A)] * 16) for n in ("k", "v", "k_scale", "v_scale")]
-    packed = ops._cache_desc(*d.values(), *[C.addressof(t) if table else 0 for t in tabs])
-    return packed, tabs
+    return (*d.values(), *[C.addressof(t) if table else 0 for t in tabs]), tabs
 
 
 def pointers(at=A):
@@ -23,13 +22,18 @@ def pointers(at=A):
 
 def append(H=4, ld_qkv=1024, ld_q=512, rot=0, rot_dim=0, cs=A, qkv=A, q=A, **kw):
     d, keep = cache(**kw)
-    st = ops._L().hydra_op_cache_append(d, H, ld_qkv, ld_q, rot, rot_dim, cs, pointers(qkv), pointers(q) if q is not None else None, None)
+    tabs = pointers(qkv), pointers(q if q is not None else A)
+    st = ops._L().hydra_op_cache_append(ops._append_desc(*d, H, ld_qkv, ld_q, rot, rot_dim, cs or 0, *[C.addressof(t) for t in tabs]), None)
     return st, lib().hydra_ops_last_error().decode()
 
 
 def attend(H=4, ld_q=512, ld_o=512, scale=0.1, q=A, o=A, lse=A, ws=None, **kw):
     d, keep = cache(**kw)
-    st = ops._L().hydra_op_cache_attention(d, H, ld_q, ld_o, 1, scale, pointers(q), pointers(o), pointers(lse), pointers(ws) if ws else None, 0, None)
+    tabs = pointers(q), pointers(o), pointers(lse), pointers(ws or A)
+    at = [C.addressof(t) for t in tabs]
+    if not ws:
+        at[3] = 0
+    st = ops._L().hydra_op_cache_attention(ops._attention_desc(*d, H, ld_q, ld_o, 1, scale, *at, 0), None)
     return st, lib().hydra_ops_last_error().decode()
 
 
@@ -57,7 +61,7 @@ def test_attention_refuses(bad):
 
 def test_attention_scratch_sizes():
     """0 for what is refused and for short sequences; the same for any number of calls; growing with the sequences."""
-    size = lambda H=4, **kw: ops._L().hydra_op_cache_attention_ws_bytes(cache(**kw)[0], H)  # noqa: E731
+    size = lambda H=4, **kw: ops._L().hydra_op_cache_attention_ws_bytes(ops._cache_desc(*cache(**kw)[0]), H)  # noqa: E731
     assert size(kind=5) == 0 and size(H=3) == 0 and size(max_len=100) == 0
     long = dict(max_pages=1000, max_len=64000)
     assert size(**long) == size(**long) > 0
@@ -72,6 +76,28 @@ def test_sample_refuses(bad):
     st = ops._L().hydra_op_sample(a["dtype"], a["rows"], a["V"], a["ldz"], a["ldu"], a["G"], pointers(a["logits"]), pointers(a["u"]), a["t"], a["k"], a["p"],
                                   a["m"], pointers(a["token"]), pointers(a["logprob"]), None)
     assert st == 1 and lib().hydra_ops_last_error().decode().startswith("hydra_op_sample: ")
+
+
+def test_descriptors_are_laid_out_as_declared():
+    """Sizes of the packed records against the C structures."""
+    ints, ptr = C.c_int, C.c_void_p
+    cache_fields = [(f"i{n}", ints) for n in range(11)] + [("page_bytes", C.c_size_t)] + [(f"p{n}", ptr) for n in range(7)]
+    desc = type("D", (C.Structure,), {"_fields_": cache_fields})
+    more = {ops._cache_desc: [], ops._append_desc: [(f"j{n}", ints) for n in range(5)] + [(f"q{n}", ptr) for n in range(3)],
+            ops._attention_desc: [(f"j{n}", ints) for n in range(4)] + [("scale", C.c_float)] + [(f"q{n}", ptr) for n in range(4)] + [("ws_bytes", C.c_size_t)]}
+    for pack, rest in more.items():
+        whole = type("W", (C.Structure,), {"_fields_": [("cache", desc)] + rest})
+        values = [1] * 11 + [2] + [3] * 7 + [0.5 if t is C.c_float else 4 for _, t in rest]
+        packed = pack(*values)
+        assert len(packed) == C.sizeof(whole)
+        w = whole.from_buffer_copy(packed)
+        assert [getattr(w.cache, n) for n, _ in cache_fields] + [getattr(w, n) for n, _ in rest] == values
+
+
+def test_null_descriptors_are_refused():
+    for f in (ops._L().hydra_op_cache_append, ops._L().hydra_op_cache_attention):
+        assert f(None, None) == 1
+    assert ops._L().hydra_op_cache_attention_ws_bytes(None, 4) == 0
 
 
 def test_cache_record_checks_its_tensors():
