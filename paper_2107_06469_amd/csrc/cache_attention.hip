@@ -118,35 +118,36 @@ struct CacheAttnPlan {
   int n_split, chunk;  // runs of keys, keys in one (a multiple of 128)
   int n_rt;            // 16-row tiles, or 128-row blocks, of the sequence with the most rows
   int page_log2;
-  bool prompt;         // many rows: cache_prompt_kernel
+  int waves;           // of a workgroup of cache_attn_kernel; 0: cache_prompt_kernel
 };
 
-// Four waves share a run of keys, 32 at a time in turn, each with its own maximum, sum and accumulators; they are joined through LDS.
+// NW waves share a run of keys, 32 at a time in turn, each with its own maximum, sum and accumulators; they are joined through LDS.
 // blockIdx: x sequence and key/value head, y run of keys and row tile, z model.
-template <int KIND, int DH>
-__global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, const CacheAttnPlan pl) {
+template <int DH, int NW>
+constexpr int attn_lds() { return NW * 16 * (DH + 4) * 4 + NW * 16 * 8; }
+template <int KIND, int DH, int NW>
+__global__ __launch_bounds__(NW * 64) void cache_attn_kernel(const CacheAttnArgs a, const CacheAttnPlan pl) {
   constexpr int W = DH / 16, NK = DH / 32, NL = DH / 64;  // bytes of a V load; k steps of a score; K loads of 16 bytes per lane
-  __shared__ float2 w_ml[4][16];
-  __shared__ __attribute__((aligned(16))) float w_o[4][16][DH + 4];
+  extern __shared__ __attribute__((aligned(16))) float w_o[];  // [NW][16][DH + 4], then the maxima and sums [NW][16]
+  float2* const w_ml = reinterpret_cast<float2*>(w_o + NW * 16 * (DH + 4));
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, gq = lane >> 4;
   const int g = blockIdx.z, b = blockIdx.x / c.HKV, h = blockIdx.x - b * c.HKV;
   const int split = blockIdx.y / pl.n_rt, rt = blockIdx.y - split * pl.n_rt;
+  const int t_lo = split * pl.chunk;
+  // lane i knows page i of a segment of 64 pages (the first one's numbers come with the lengths, whatever these are)
+  auto page_at = [&](int seg) {
+    const int i = (seg >> pl.page_log2) + lane;
+    return i < c.max_pages ? c.table[(size_t)b * c.max_pages + i] : -1;
+  };
+  const int first_pages = page_at(t_lo);
   const CacheSeq sq = cache_seq(c, b);
   const int share = a.H / c.HKV, rows = sq.n * share, first = rt * 16;
   if (first >= rows) return;
   const int all = a.causal ? max(sq.pos0 + (min(first + 16, rows) - 1) / share + 1, 0) : sq.len;  // keys that the tile's last row sees
-  const int t_lo = split * pl.chunk, t_hi = min(t_lo + pl.chunk, all);
-  // lane i knows page i of a segment of 64 pages; the first one's ids and the queries are asked for together
-  auto page_of = [&](int seg) {
-    int id = -1;
-    if (seg + (lane << pl.page_log2) < t_hi) {
-      id = c.table[(size_t)b * c.max_pages + (seg >> pl.page_log2) + lane];
-      id = (unsigned)id < (unsigned)c.n_pages ? id : -1;
-    }
-    return id;
-  };
-  int id = page_of(t_lo);
+  const int t_hi = min(t_lo + pl.chunk, all);
+  auto page_of = [&](int seg, int id) { return seg + (lane << pl.page_log2) < t_hi && (unsigned)id < (unsigned)c.n_pages ? id : -1; };
+  int id = page_of(t_lo, first_pages);
   // this lane's row
   const bool have = first + r < rows;
   const int row = have ? first + r : first, j = row / share, hq = h * share + row - j * share;
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
   for (int seg = t_lo; seg < t_hi; seg += 64 << pl.page_log2) {
     const int seg_hi = min(t_hi, seg + (64 << pl.page_log2));
     if (seg > t_lo) {
-      id = page_of(seg);
+      id = page_of(seg, page_at(seg));
       scales();
       if (seg + wave * 32 < seg_hi) fetch(t0, seg, seg + wave * 32);
     }
@@ -315,54 +316,56 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
     };
     int t = seg + wave * 32;
     Tile t1;  // one tile ahead: what a wave waits for was asked for a tile ago
-    for (; t < seg_hi; t += 256) {
-      if (t + 128 < seg_hi) fetch(t1, seg, t + 128);
+    constexpr int STEP = NW * 32;
+    for (; t < seg_hi; t += 2 * STEP) {
+      if (t + STEP < seg_hi) fetch(t1, seg, t + STEP);
       use(t0, t);
-      if (t + 128 < seg_hi) {
-        if (t + 256 < seg_hi) fetch(t0, seg, t + 256);
-        use(t1, t + 128);
+      if (t + STEP < seg_hi) {
+        if (t + 2 * STEP < seg_hi) fetch(t0, seg, t + 2 * STEP);
+        use(t1, t + STEP);
       }
     }
   }
   l = quarter_sum(l) * (1.0f / P_ONE);
   const float one = unit * (KIND == CACHE_INT8 ? U_ONE / P_ONE : 1.0f / P_ONE);
 
-  if (gq == 0) w_ml[wave][r] = make_float2(m, l);
+  if (gq == 0) w_ml[wave * 16 + r] = make_float2(m, l);
 #pragma unroll
   for (int e = 0; e < 4; ++e)
 #pragma unroll
     for (int i = 0; i < W; i += 4) {
       const f32x4 v = f32x4{acc[i][e], acc[i + 1][e], acc[i + 2][e], acc[i + 3][e]};
-      *reinterpret_cast<f32x4*>(&w_o[wave][r][W * (4 * gq + e) + i]) = v * one;
+      *reinterpret_cast<f32x4*>(w_o + (wave * 16 + r) * (DH + 4) + W * (4 * gq + e) + i) = v * one;
     }
   __syncthreads();
-  const int jr = tid >> 4, at = tid & 15, d0 = at * W;  // joined by 16 threads a row, W columns each
+  constexpr int C = W * 4 / NW, PER_ROW = 4 * NW;  // joined by PER_ROW threads a row, C columns each
+  const int jr = tid / PER_ROW, at = tid % PER_ROW, d0 = at * C;
   if (first + jr >= rows) return;
   float mm = NEG_BIG;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) mm = fmaxf(mm, w_ml[w][jr].x);
-  float ll = 0.f, o[W];
+  for (int w = 0; w < NW; ++w) mm = fmaxf(mm, w_ml[w * 16 + jr].x);
+  float ll = 0.f, o[C];
 #pragma unroll
-  for (int i = 0; i < W; ++i) o[i] = 0.f;
+  for (int i = 0; i < C; ++i) o[i] = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float f = fast_exp2(w_ml[w][jr].x - mm);
-    ll += w_ml[w][jr].y * f;
+  for (int w = 0; w < NW; ++w) {
+    const float f = fast_exp2(w_ml[w * 16 + jr].x - mm);
+    ll += w_ml[w * 16 + jr].y * f;
 #pragma unroll
-    for (int i = 0; i < W; ++i) o[i] += w_o[w][jr][d0 + i] * f;
+    for (int i = 0; i < C; ++i) o[i] += w_o[(w * 16 + jr) * (DH + 4) + d0 + i] * f;
   }
   const int tok = sq.row0 + (first + jr) / share, head = h * share + (first + jr) % share;
   if (pl.n_split == 1) {
     const float f = ll > 0.f ? 1.0f / ll : (ll == 0.f ? 0.f : ll);
     uint32_t* dst = reinterpret_cast<uint32_t*>(a.o[g] + (size_t)tok * a.ld_o + (size_t)head * DH + d0);
 #pragma unroll
-    for (int i = 0; i < W; i += 2) dst[i >> 1] = pack_bf16(o[i] * f, o[i + 1] * f);
+    for (int i = 0; i < C; i += 2) dst[i >> 1] = pack_bf16(o[i] * f, o[i + 1] * f);
     if (a.lse[g] && at == 0) a.lse[g][(size_t)tok * a.H + head] = ll > 0.f ? mm * LN2 + __logf(ll) : (ll == 0.f ? -__builtin_inff() : ll);
   } else {
     const size_t part = ((size_t)tok * a.H + head) * pl.n_split + split;
     float* po = static_cast<float*>(a.ws[g]) + part * DH + d0;
 #pragma unroll
-    for (int i = 0; i < W; ++i) po[i] = o[i];
+    for (int i = 0; i < C; ++i) po[i] = o[i];
     float2* ml = reinterpret_cast<float2*>(static_cast<float*>(a.ws[g]) + (size_t)c.n_tok * a.H * pl.n_split * DH);
     if (at == 0) ml[part] = make_float2(mm, ll);
   }
@@ -373,7 +376,9 @@ __global__ __launch_bounds__(256) void cache_attn_kernel(const CacheAttnArgs a, 
 // chunk and transposing reads both spread over the banks): codes are widened once for all of a workgroup's rows on their way there.  The
 // next tile's codes are in registers while this one's products run; one barrier a tile.  v_mfma_f32_32x32x16_f16:
 //   S^T[t,i] = K Q^T (lane: query l%32; accumulator rows 8q + 4(l/32) + e),  O^T[d,i] += V^T P^T, P from the accumulators as they are, V^T by transposing
-//   LDS reads.  Values carry 2^7 of their page's scale in units of the window's largest, weights 2^7 or more, so that f16 holds small ones.
+//   LDS reads.  A
+// page's scale of the keys is in the factor of its scores, that of the values, in units of the window's largest one, in the exponent of its
+// weights (their own sum takes it back): neither costs an instruction a score.  Weights carry 2^7 besides, so that f16 holds small ones.
 // What a window of 512 pages is (id and scales) waits in LDS, too.
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 __device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, f32x16 c) {
@@ -401,32 +406,28 @@ __device__ __forceinline__ uint4 read_columns(const ColumnsAt& c, unsigned off) 
   const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(c.a1 + off)));
   return make_uint4(lo.x, lo.y, hi.x, hi.y);
 }
-// What wide8 gives as values times f: u as 1024 + u (the exponent goes beside it), less 1152
+// What wide8 gives, of int8 without the 128: code 2^-24
 template <int KIND>
-__device__ __forceinline__ uint4 value_of(const uint4& v, uint32_t f) {
-  const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
-  auto one = [&](uint32_t w) {
-    if (KIND == CACHE_INT8) w = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, w | 0x64006400u) - off);
-    return times2(w, f);
-  };
+__device__ __forceinline__ uint4 codes_only(const uint4& v) {
+  if (KIND == CACHE_E4M3) return v;
+  auto one = [](uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, w) + __builtin_bit_cast(f16x2, 0x80808080u)); };
   return make_uint4(one(v.x), one(v.y), one(v.z), one(v.w));
 }
 constexpr int WINDOW = 512;
 template <int DH>
-constexpr int prompt_lds() { return 2 * 2 * 64 * DH * 2 + 3 * WINDOW * 4 + 64; }
+constexpr int prompt_lds() { return 2 * 2 * 64 * DH * 2 + 4 * WINDOW * 4; }
 
 // blockIdx: x sequence and key/value head (the blocks of one head run on one XCD where their number is a multiple of 8), y run of keys and row block, the
-// last (longest) row blocks first; z model.
-template <int KIND, int DH, int NW>
+// last (longest) row blocks first; z model.  BIG: a tile lies in one page.
+template <int KIND, int DH, int NW, bool BIG>
 __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAttnArgs a, const CacheAttnPlan pl) {
   constexpr int NT = NW * 64, NCH = DH / 8, NK = DH / 16, NC = DH / 32, BUF = 2 * 64 * NCH;  // chunks of a buffer: K, then V
   constexpr int LOADS = 2 * 64 * (DH / 16) / NT;                                             // of 16 codes per thread and tile
   extern __shared__ __attribute__((aligned(256))) uint4 lds[];
   int* const s_id = reinterpret_cast<int*>(lds + 2 * BUF);
   float* const s_ks = reinterpret_cast<float*>(s_id + WINDOW);
-  float* const s_vs = s_ks + WINDOW;
-  uint32_t* const s_vf = reinterpret_cast<uint32_t*>(s_vs);
-  int* const s_bad = reinterpret_cast<int*>(s_vs + WINDOW);
+  float* const s_vs = s_ks + WINDOW;  // of values: the scale, then its log2 in units of the window's largest
+  float* const s_vi = s_vs + WINDOW;  // 2^ less that
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 31, g = lane >> 5;
   const int gi = blockIdx.z, b = blockIdx.x / c.HKV, h = blockIdx.x - b * c.HKV;
@@ -492,18 +493,15 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
     for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
   float m = NEG_BIG, l = 0.f, unit = 0.f;
   int win = 0;       // the window's first page
-  bool bad = false;  // some page of the window is not there
   auto window = [&](int key) {
     win = key >> pl.page_log2;
-    __syncthreads();
-    if (tid == 0) *s_bad = 0;
     __syncthreads();
     for (int p = tid; p < WINDOW; p += NT) {
       int id = -1;
       float ks = 0.f, vs = 0.f;
       if (((int64_t)(win + p) << pl.page_log2) < t_hi) {
         id = c.table[(size_t)b * c.max_pages + win + p];
-        if ((unsigned)id >= (unsigned)c.n_pages) id = -1, *s_bad = 1;
+        if ((unsigned)id >= (unsigned)c.n_pages) id = -1;
         else ks = c.ks[gi][(size_t)id * c.HKV + h], vs = c.vs[gi][(size_t)id * c.HKV + h];
       }
       s_id[p] = id, s_ks[p] = ks, s_vs[p] = vs;
@@ -518,122 +516,173 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
       for (int i = 0; i < NC; ++i) acc[i] *= again;
     }
     unit = most;
-    bad = *s_bad != 0;
     __syncthreads();  // every wave has read the scales
     for (int p = tid; p < WINDOW; p += NT) {
-      const float f = unit > 0.f ? s_vs[p] / unit * 128.f : 0.f;
-      s_vf[p] = pack_f16(f, f);
+      const float f = unit > 0.f ? fmaxf(s_vs[p] / unit, 0x1p-40f) : 1.f;  // (2^-40 of the largest is nothing)
+      s_vs[p] = __builtin_amdgcn_logf(f), s_vi[p] = 1.0f / f;
     }
     __syncthreads();
   };
   uint4 raw[LOADS];
-  uint32_t vf[LOADS];
   // load i of this thread: 16 codes of a tile's keys or (is_v: whole waves) values
   constexpr int CODES = 64 * (DH / 16);
   auto is_v = [&](int i) { return (i * NW + wave) * 64 >= CODES; };
-  auto fetch = [&](int t) {
+  // (neighbouring rows of a tile would write to the same banks: rows r and r + 4 are neighbours here)
+  auto row_of = [&](int i) {
+    const int q = ((i * NT + tid) & (CODES - 1)) / (DH / 16);
+    return (q & ~7) | (q & 1) << 2 | (q >> 1 & 3);
+  };
+  auto col_of = [&](int i) { return tid & (DH / 16 - 1); };
+  // What the scalar unit knows of a tile: its pages (of 16 keys each, or the one).  Asked for a tile ahead, like the codes.
+  constexpr int NG = BIG ? 1 : 4;
+  struct Pages { int id[NG]; float ks[NG], lv[NG], iv[NG]; };
+  auto pages_at = [&](int t) {
+    Pages p;
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int at = (i * NT + tid) & (CODES - 1), r = at / (DH / 16), c16 = at & (DH / 16 - 1);
-      const int key = t + r, pg = (key >> pl.page_log2) - win, pid = key < t_hi ? s_id[pg] : -1;
-      const uint8_t* p = (is_v(i) ? c.v[gi] : c.k[gi]) + (size_t)max(pid, 0) * c.page_bytes + ((size_t)h * c.page + (key & (c.page - 1))) * DH + c16 * 16;
-      raw[i] = pid >= 0 ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
-      if (is_v(i)) vf[i] = pid >= 0 ? s_vf[pg] : 0u;
+    for (int x = 0; x < NG; ++x) {
+      const int at = min(((t + 16 * x) >> pl.page_log2) - win, WINDOW - 1);
+      p.id[x] = s_id[at], p.ks[x] = s_ks[at], p.lv[x] = s_vs[at], p.iv[x] = s_vi[at];
+    }
+    return p;
+  };
+  auto settle = [&](const Pages& v) {
+    Pages p;
+    auto one = [](float f) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(f))); };
+#pragma unroll
+    for (int x = 0; x < NG; ++x) p.id[x] = __builtin_amdgcn_readfirstlane(v.id[x]), p.ks[x] = one(v.ks[x]), p.lv[x] = one(v.lv[x]), p.iv[x] = one(v.iv[x]);
+    return p;
+  };
+  auto fetch = [&](int t, const Pages& pg) {
+    if constexpr (BIG) {
+      const int id = pg.id[0];
+      const size_t at = (size_t)max(id, 0) * c.page_bytes + ((size_t)h * c.page + (t & (c.page - 1))) * DH;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) raw[i] = *reinterpret_cast<const uint4*>((is_v(i) ? c.v[gi] : c.k[gi]) + at + (unsigned)(row_of(i) * DH + col_of(i) * 16));
+      if (KIND == CACHE_E4M3 && (id < 0 || t + 64 > t_hi)) {  // what no token has written may be a NaN
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          if (id < 0 || t + row_of(i) >= t_hi) raw[i] = make_uint4(0, 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int key = t + row_of(i), pid = key < t_hi ? s_id[(key >> pl.page_log2) - win] : -1;
+        const uint8_t* p = (is_v(i) ? c.v[gi] : c.k[gi]) + (size_t)max(pid, 0) * c.page_bytes + ((size_t)h * c.page + (key & (c.page - 1))) * DH + col_of(i) * 16;
+        raw[i] = pid >= 0 ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
+      }
     }
   };
   auto put = [&](uint4* tile) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int at = (i * NT + tid) & (CODES - 1), r = at / (DH / 16), c16 = at & (DH / 16 - 1);
+      const int r = row_of(i), kc = 2 * col_of(i);
       uint4 lo = wide8<KIND>(raw[i].x, raw[i].y), hi = wide8<KIND>(raw[i].z, raw[i].w);
       uint4* p = tile + r * NCH;
-      if (is_v(i)) lo = value_of<KIND>(lo, vf[i]), hi = value_of<KIND>(hi, vf[i]), p += 64 * NCH;
-      p[(2 * c16) ^ swz<DH>(r)] = lo;
-      p[(2 * c16 + 1) ^ swz<DH>(r)] = hi;
+      if (is_v(i)) lo = codes_only<KIND>(lo), hi = codes_only<KIND>(hi), p += 64 * NCH;
+      p[kc ^ swz<DH>(r)] = lo;
+      p[(kc + 1) ^ swz<DH>(r)] = hi;
     }
   };
 
+  Pages now{}, next{};
   if (t_lo < t_hi) {
     window(t_lo);
-    fetch(t_lo);
+    now = settle(pages_at(t_lo)), next = settle(pages_at(t_lo + 64));
+    fetch(t_lo, now);
     put(lds);
     __syncthreads();
   }
   auto tile = [&](auto buf_, int t) {
     constexpr int B = decltype(buf_)::value * BUF;
-    const bool more = t + 64 < t_hi;
-    float fk[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) fk[x] = s_ks[min(((t + 16 * x) >> pl.page_log2) - win, WINDOW - 1)] * q_scale;
+    const bool more = t + 64 < t_hi, turn = more && ((t + 64 + 63) >> pl.page_log2) - win >= WINDOW;
+    if (more && !turn) fetch(t + 64, next);
     unsigned gone = 0;  // 16-key groups that are not there
-    if (bad) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) gone |= s_id[min(((t + 16 * x) >> pl.page_log2) - win, WINDOW - 1)] < 0 ? 1u << x : 0u;
-    }
-    const bool turn = more && ((t + 64 + 63) >> pl.page_log2) - win >= WINDOW;
-    if (more && !turn) fetch(t + 64);
+    for (int x = 0; x < NG; ++x) gone |= now.id[x] < 0 ? (BIG ? 15u : 1u << x) : 0u;
     if (t < wave_all) {
-      f32x16 s[2];
+      // 32 keys at a time, so that the products of one half stand beside the exponentials of the other
+      const bool edge = t + 64 > wave_free || gone;
+      f32x16 s;
+      auto scores = [&](int sub) {
 #pragma unroll
-      for (int sub = 0; sub < 2; ++sub) {
+        for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[sub][e] = begin;
+        for (int k = 0; k < NK; ++k) s = mfma32(kr[k][B + sub * 32 * NCH], qf[k], s);
+      };
+      float f[2], start = begin;
+      auto highest = [&](int sub) {  // and the masks; masked scores are scaled at once
+        float top = NEG_BIG;
+        f[0] = now.ks[2 * sub % NG] * q_scale, f[1] = now.ks[(2 * sub + 1) % NG] * q_scale;
+        if (edge) {
+          const int left = min(sees, t_hi) - t - 4 * g;
 #pragma unroll
-        for (int k = 0; k < NK; ++k) s[sub] = mfma32(kr[k][B + sub * 32 * NCH], qf[k], s[sub]);
-      }
-      float top = NEG_BIG;
-      if (t + 64 > wave_free || gone) {  // masked, and scaled here already
-        const int left = min(sees, t_hi) - t - 4 * g;
+          for (int x = 0; x < 2; ++x) {
+            const int here = gone >> (2 * sub + x) & 1 ? 0 : left;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int here = gone >> x & 1 ? 0 : left;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float z = 16 * x + 8 * (e >> 2) + (e & 3) < here ? s[x >> 1][8 * (x & 1) + e] * fk[x] : -__builtin_inff();
-            s[x >> 1][8 * (x & 1) + e] = z;
-            top = fmaxf(top, z);
+            for (int e = 0; e < 8; ++e) {
+              const float z = 16 * (2 * sub + x) + 8 * (e >> 2) + (e & 3) < here ? (s[8 * x + e] + begin) * f[x] : -__builtin_inff();
+              s[8 * x + e] = z;
+              top = fmaxf(top, z);
+            }
+            f[x] = 1.f;
           }
-          fk[x] = 1.f;
+          start = 0.f;
+        } else {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            float most = s[8 * x];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) most = fmaxf(most, s[8 * x + e]);
+            top = fmaxf(top, (most + start) * f[x]);
+          }
         }
-      } else {
+        const float2 both = wave_swap32(top);
+        top = fmaxf(both.x, both.y);
+        // weights are 2^7 of those by the maximum that is held: it may lag by 2^8 (their f16 ends at 2^16) before accumulators are scaled again
+        if (__any(top > m + 8.f)) {
+          top = fmaxf(top, m);
+          const float keep = fast_exp2(m - top);
+          l *= keep;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          float big = s[x >> 1][8 * (x & 1)];
-#pragma unroll
-          for (int e = 1; e < 8; ++e) big = fmaxf(big, s[x >> 1][8 * (x & 1) + e]);
-          top = fmaxf(top, big * fk[x]);
+          for (int i = 0; i < NC; ++i) acc[i] *= keep;
+          m = top;
         }
-      }
-      const float2 both = wave_swap32(top);
-      top = fmaxf(both.x, both.y);
-      // weights are 2^7 of those by the maximum that is held: it may lag by 2^8 (their f16 ends at 2^16) before accumulators are scaled again
-      if (__any(top > m + 8.f)) {
-        top = fmaxf(top, m);
-        const float keep = fast_exp2(m - top);
-        l *= keep;
+      };
+      uint4 pf[2];
+      auto weights = [&](int sub) {
 #pragma unroll
-        for (int i = 0; i < NC; ++i) acc[i] *= keep;
-        m = top;
-      }
-      const float off = 7.f - m;
-      float sum[4];
+        for (int x = 0; x < 2; ++x) {
+          float p[8];
+          const float off = fmaf(start, f[x], 7.f - m + now.lv[(2 * sub + x) % NG]);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        float p[8];
+          for (int e = 0; e < 8; ++e) p[e] = fast_exp2(fmaf(s[8 * x + e], f[x], off));
+          l += (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]))) * now.iv[(2 * sub + x) % NG];
+          pf[x] = make_uint4(pack_f16(p[0], p[1]), pack_f16(p[2], p[3]), pack_f16(p[4], p[5]), pack_f16(p[6], p[7]));
+        }
+      };
+      auto results = [&](int sub) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = fast_exp2(fmaf(s[x >> 1][8 * (x & 1) + e], fk[x], off));
-        sum[x] = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-        const uint4 pf = make_uint4(pack_f16(p[0], p[1]), pack_f16(p[2], p[3]), pack_f16(p[4], p[5]), pack_f16(p[6], p[7]));
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int i = 0; i < NC; ++i) acc[i] = mfma32(read_columns(vc[i], (unsigned)((B + 16 * x * NCH) * 16)), pf, acc[i]);
-      }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          for (int i = 0; i < NC; ++i) acc[i] = mfma32(read_columns(vc[i], (unsigned)((B + (2 * sub + x) * 16 * NCH) * 16)), pf[x], acc[i]);
+      };
+      scores(0);
+      highest(0);
+      weights(0);
+      scores(1);
+      results(0);
+      highest(1);
+      weights(1);
+      results(1);
     }
     if (turn) {
       window(t + 64);
-      fetch(t + 64);
+      next = settle(pages_at(t + 64));
+      fetch(t + 64, next);
     }
+    const Pages then = pages_at(t + 128);
     if (more) put(lds + (BUF - B));
+    now = next, next = settle(then);
     __syncthreads();
   };
   for (int t = t_lo; t < t_hi; t += 128) {
@@ -644,7 +693,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
   const float2 both = wave_swap32(l);
   l = (both.x + both.y) * (1.0f / 128.f);
   if (row >= rows) return;
-  const float one = unit * (1.0f / 128.f / 128.f);
+  const float one = unit * (KIND == CACHE_INT8 ? U_ONE / 128.f : 1.0f / 128.f);
   const int tok = sq.row0 + j;
   if (pl.n_split == 1) {
     const float f = l > 0.f ? one / l : (l == 0.f ? 0.f : l);
@@ -717,12 +766,16 @@ CacheAttnPlan plan_of(const CacheArgs& c, int H) {
   CacheAttnPlan p{};
   p.page_log2 = floor_log2(c.page);
   const int64_t rows = (int64_t)c.max_q * (H / c.HKV), len = c.max_len;
-  p.prompt = rows > 64;
-  p.n_rt = (int)((rows + (p.prompt ? 127 : 15)) / (p.prompt ? 128 : 16));
-  const int64_t base = (int64_t)c.G * c.B * c.HKV * p.n_rt;
+  const int64_t heads = (int64_t)c.G * c.B * c.HKV, tiles = heads * ((rows + 15) / 16);
+  p.waves = rows > 64 && (tiles > 256 || len > 8192) ? 0 : tiles <= 512 ? 8 : 4;
+  p.n_rt = (int)((rows + (p.waves ? 15 : 127)) / (p.waves ? 16 : 128));
+  const int64_t base = heads * p.n_rt;
   int64_t n;
-  if (p.prompt) n = std::min((256 + base - 1) / base, (len + 511) / 512);
-  else n = len <= 640 ? 1 : std::min(std::max((512 + base - 1) / base, (len + 4095) / 4096), (len + 127) / 128);
+  if (!p.waves) {
+    n = std::min((512 + base - 1) / base, (len + 255) / 256);
+  } else {
+    n = len <= 640 ? 1 : std::min(std::max(256 / base, (len + 8191) / 8192), (len + 255) / 256);
+  }
   p.chunk = (int)(((len + n - 1) / n + 127) / 128 * 128);
   p.n_split = (int)((len + p.chunk - 1) / p.chunk);
   return p;
@@ -730,13 +783,19 @@ CacheAttnPlan plan_of(const CacheArgs& c, int H) {
 
 template <int KIND, int DH>
 hipError_t run_attn(const CacheAttnArgs& a, const CacheAttnPlan& p, dim3 grid, hipStream_t s) {
-  if (p.prompt) hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH, 4>), grid, dim3(256), prompt_lds<DH>(), s, a, p);
-  else hipLaunchKernelGGL((cache_attn_kernel<KIND, DH>), grid, dim3(256), 0, s, a, p);
+  if (!p.waves && p.page_log2 >= 6) hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH, 4, true>), grid, dim3(256), prompt_lds<DH>(), s, a, p);
+  else if (!p.waves) hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH, 4, false>), grid, dim3(256), prompt_lds<DH>(), s, a, p);
+  else if (p.waves == 4) hipLaunchKernelGGL((cache_attn_kernel<KIND, DH, 4>), grid, dim3(256), (attn_lds<DH, 4>()), s, a, p);
+  else hipLaunchKernelGGL((cache_attn_kernel<KIND, DH, 8>), grid, dim3(512), (attn_lds<DH, 8>()), s, a, p);
   return hipGetLastError();
 }
 template <int KIND, int DH>
 hipError_t attn_init_kind() {
-  return hipFuncSetAttribute((const void*)cache_prompt_kernel<KIND, DH, 4>, hipFuncAttributeMaxDynamicSharedMemorySize, prompt_lds<DH>());
+  hipError_t e = hipFuncSetAttribute((const void*)cache_attn_kernel<KIND, DH, 8>, hipFuncAttributeMaxDynamicSharedMemorySize, attn_lds<DH, 8>());
+  if (e != hipSuccess) return e;
+  e = hipFuncSetAttribute((const void*)cache_prompt_kernel<KIND, DH, 4, false>, hipFuncAttributeMaxDynamicSharedMemorySize, prompt_lds<DH>());
+  if (e != hipSuccess) return e;
+  return hipFuncSetAttribute((const void*)cache_prompt_kernel<KIND, DH, 4, true>, hipFuncAttributeMaxDynamicSharedMemorySize, prompt_lds<DH>());
 }
 
 }  // namespace
