@@ -413,6 +413,10 @@ __device__ __forceinline__ uint4 codes_only(const uint4& v) {
   auto one = [](uint32_t w) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, w) + __builtin_bit_cast(f16x2, 0x80808080u)); };
   return make_uint4(one(v.x), one(v.y), one(v.z), one(v.w));
 }
+__device__ __forceinline__ void store16(uint4* p, const uint4& v) {
+  typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+  *reinterpret_cast<u32x4*>(p) = u32x4{v.x, v.y, v.z, v.w};
+}
 constexpr int WINDOW = 512;
 template <int DH>
 constexpr int prompt_lds() { return 2 * 2 * 64 * DH * 2 + 4 * WINDOW * 4; }
@@ -437,9 +441,10 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
   if (first >= rows) return;
   auto sees_of = [&](int row) { return row < rows ? (a.causal ? max(sq.pos0 + row / share + 1, 0) : sq.len) : 0; };
   const int row = first + wave * 32 + li, sees = sees_of(row), rc = min(row, rows - 1), j = rc / share, hq = h * share + rc - j * share;
-  const int t_lo = split * pl.chunk, t_hi = min(t_lo + pl.chunk, sees_of(min(first + NW * 32, rows) - 1));
-  const int wave_last = min(first + wave * 32 + 32, rows) - 1, wave_all = first + wave * 32 < rows ? min(sees_of(wave_last), t_hi) : 0;
-  const int wave_free = first + wave * 32 + 32 <= rows ? min(sees_of(first + wave * 32), t_hi) : 0;  // keys that all of the wave's rows see
+  auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  const int t_lo = split * pl.chunk, t_hi = uniform(min(t_lo + pl.chunk, sees_of(min(first + NW * 32, rows) - 1)));
+  const int wave_last = min(first + wave * 32 + 32, rows) - 1, wave_all = uniform(first + wave * 32 < rows ? min(sees_of(wave_last), t_hi) : 0);
+  const int wave_free = uniform(first + wave * 32 + 32 <= rows ? min(sees_of(first + wave * 32), t_hi) : 0);  // keys that all of the wave's rows see
 
   uint4 qf[NK];
   float q_scale;
@@ -524,9 +529,10 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
     __syncthreads();
   };
   uint4 raw[LOADS];
-  // load i of this thread: 16 codes of a tile's keys or (is_v: whole waves) values
+  // load i of this thread: 16 codes of a tile's keys or, from KEY_LOADS on, values
   constexpr int CODES = 64 * (DH / 16);
-  auto is_v = [&](int i) { return (i * NW + wave) * 64 >= CODES; };
+  static_assert(CODES % NT == 0, "a load is one of keys for all threads, or one of values");
+  constexpr int KEY_LOADS = CODES / NT;
   // (neighbouring rows of a tile would write to the same banks: rows r and r + 4 are neighbours here)
   auto row_of = [&](int i) {
     const int q = ((i * NT + tid) & (CODES - 1)) / (DH / 16);
@@ -557,7 +563,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
       const int id = pg.id[0];
       const size_t at = (size_t)max(id, 0) * c.page_bytes + ((size_t)h * c.page + (t & (c.page - 1))) * DH;
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) raw[i] = *reinterpret_cast<const uint4*>((is_v(i) ? c.v[gi] : c.k[gi]) + at + (unsigned)(row_of(i) * DH + col_of(i) * 16));
+      for (int i = 0; i < LOADS; ++i) raw[i] = *reinterpret_cast<const uint4*>((i < KEY_LOADS ? c.k[gi] : c.v[gi]) + at + (unsigned)(row_of(i) * DH + col_of(i) * 16));
       if (KIND == CACHE_E4M3 && (id < 0 || t + 64 > t_hi)) {  // what no token has written may be a NaN
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
@@ -567,7 +573,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
         const int key = t + row_of(i), pid = key < t_hi ? s_id[(key >> pl.page_log2) - win] : -1;
-        const uint8_t* p = (is_v(i) ? c.v[gi] : c.k[gi]) + (size_t)max(pid, 0) * c.page_bytes + ((size_t)h * c.page + (key & (c.page - 1))) * DH + col_of(i) * 16;
+        const uint8_t* p = (i < KEY_LOADS ? c.k[gi] : c.v[gi]) + (size_t)max(pid, 0) * c.page_bytes + ((size_t)h * c.page + (key & (c.page - 1))) * DH + col_of(i) * 16;
         raw[i] = pid >= 0 ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
       }
     }
@@ -578,24 +584,18 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
       const int r = row_of(i), kc = 2 * col_of(i);
       uint4 lo = wide8<KIND>(raw[i].x, raw[i].y), hi = wide8<KIND>(raw[i].z, raw[i].w);
       uint4* p = tile + r * NCH;
-      if (is_v(i)) lo = codes_only<KIND>(lo), hi = codes_only<KIND>(hi), p += 64 * NCH;
-      p[kc ^ swz<DH>(r)] = lo;
-      p[(kc + 1) ^ swz<DH>(r)] = hi;
+      if (i >= KEY_LOADS) lo = codes_only<KIND>(lo), hi = codes_only<KIND>(hi), p += 64 * NCH;
+      store16(p + (kc ^ swz<DH>(r)), lo);
+      store16(p + ((kc + 1) ^ swz<DH>(r)), hi);
     }
   };
 
   Pages now{}, next{};
-  if (t_lo < t_hi) {
-    window(t_lo);
-    now = settle(pages_at(t_lo)), next = settle(pages_at(t_lo + 64));
-    fetch(t_lo, now);
-    put(lds);
-    __syncthreads();
-  }
+  int w_hi = 0;  // the end of the window's keys
   auto tile = [&](auto buf_, int t) {
     constexpr int B = decltype(buf_)::value * BUF;
-    const bool more = t + 64 < t_hi, turn = more && ((t + 64 + 63) >> pl.page_log2) - win >= WINDOW;
-    if (more && !turn) fetch(t + 64, next);
+    const bool more = t + 64 < w_hi;
+    if (more) fetch(t + 64, next);
     unsigned gone = 0;  // 16-key groups that are not there
 #pragma unroll
     for (int x = 0; x < NG; ++x) gone |= now.id[x] < 0 ? (BIG ? 15u : 1u << x) : 0u;
@@ -675,19 +675,22 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
       weights(1);
       results(1);
     }
-    if (turn) {
-      window(t + 64);
-      next = settle(pages_at(t + 64));
-      fetch(t + 64, next);
-    }
     const Pages then = pages_at(t + 128);
     if (more) put(lds + (BUF - B));
     now = next, next = settle(then);
     __syncthreads();
   };
-  for (int t = t_lo; t < t_hi; t += 128) {
-    tile(std::integral_constant<int, 0>{}, t);
-    if (t + 64 < t_hi) tile(std::integral_constant<int, 1>{}, t + 64);
+  for (int w = t_lo; w < t_hi; w = w_hi) {
+    w_hi = uniform((int)min((int64_t)t_hi, (int64_t)w + ((int64_t)WINDOW << pl.page_log2)));
+    window(w);
+    now = settle(pages_at(w)), next = settle(pages_at(w + 64));
+    fetch(w, now);
+    put(lds);
+    __syncthreads();
+    for (int t = w; t < w_hi; t += 128) {
+      tile(std::integral_constant<int, 0>{}, t);
+      if (t + 64 < w_hi) tile(std::integral_constant<int, 1>{}, t + 64);
+    }
   }
 
   const float2 both = wave_swap32(l);
