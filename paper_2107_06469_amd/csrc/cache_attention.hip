@@ -500,8 +500,10 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
   int win = 0;       // the window's first page
   auto window = [&](int key) {
     win = key >> pl.page_log2;
+    // as many pages as the tiles ask for, two ahead of the last one
+    const int n = uniform((int)min((int64_t)WINDOW, (((int64_t)t_hi - key + 191) >> pl.page_log2) + 1));
     __syncthreads();
-    for (int p = tid; p < WINDOW; p += NT) {
+    for (int p = tid; p < n; p += NT) {
       int id = -1;
       float ks = 0.f, vs = 0.f;
       if (((int64_t)(win + p) << pl.page_log2) < t_hi) {
@@ -513,7 +515,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
     }
     __syncthreads();
     float most = unit;
-    for (int p = lane; p < WINDOW; p += 64) most = fmaxf(most, s_vs[p]);
+    for (int p = lane; p < n; p += 64) most = fmaxf(most, s_vs[p]);
     most = wave_max(most);
     const float again = most > 0.f ? unit / most : 0.f;
     if (unit > 0.f && again != 1.f) {
@@ -522,7 +524,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
     }
     unit = most;
     __syncthreads();  // every wave has read the scales
-    for (int p = tid; p < WINDOW; p += NT) {
+    for (int p = tid; p < n; p += NT) {
       const float f = unit > 0.f ? fmaxf(s_vs[p] / unit, 0x1p-40f) : 1.f;  // (2^-40 of the largest is nothing)
       s_vs[p] = __builtin_amdgcn_logf(f), s_vi[p] = 1.0f / f;
     }
@@ -603,11 +605,17 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
       // 32 keys at a time, so that the products of one half stand beside the exponentials of the other
       const bool edge = t + 64 > wave_free || gone;
       f32x16 s;
-      auto scores = [&](int sub) {
+      uint4 kf[NK];
+      auto keys = [&](int sub) {  // all fragments asked for at once (left alone, each read is waited for where it stands)
+#pragma unroll
+        for (int k = 0; k < NK; ++k) kf[k] = kr[k][B + sub * 32 * NCH];
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      auto scores = [&] {
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
-        for (int k = 0; k < NK; ++k) s = mfma32(kr[k][B + sub * 32 * NCH], qf[k], s);
+        for (int k = 0; k < NK; ++k) s = mfma32(kf[k], qf[k], s);
       };
       float f[2], start = begin;
       auto highest = [&](int sub) {  // and the masks; masked scores are scaled at once
@@ -666,10 +674,12 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
 #pragma unroll
           for (int i = 0; i < NC; ++i) acc[i] = mfma32(read_columns(vc[i], (unsigned)((B + (2 * sub + x) * 16 * NCH) * 16)), pf[x], acc[i]);
       };
-      scores(0);
+      keys(0);
+      scores();
+      keys(1);
       highest(0);
       weights(0);
-      scores(1);
+      scores();
       results(0);
       highest(1);
       weights(1);
