@@ -12,7 +12,6 @@
 // and the draw look at nothing else.  Up to 128 of them are ranked directly; of more, or over the whole row, the bin is the next round's range
 // until 256 tokens at most are left in it (equal logits are told apart by histograms over their indices).
 #include <float.h>
-#include <type_traits>
 
 #include "kernels.h"
 #include "wave_math.h"
@@ -86,44 +85,56 @@ struct Row {
     if constexpr (VEC == 4) return logit(i < n_lds * VEC ? reinterpret_cast<const float*>(lds)[i] : p[i]);
     else return logit(__uint_as_float((uint32_t)(i < n_lds * VEC ? reinterpret_cast<const bf16_t*>(lds)[i] : p[i]) << 16));
   }
-  template <bool FIX, typename F>
-  static __device__ __forceinline__ void tokens(const uint4& v, int q, F& f) {
+  // NaN to -inf and +inf to the largest number, in a run
+  static __device__ __forceinline__ uint4 mended(uint4 v) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (VEC == 4) {
+        w[e] = __float_as_uint(logit(__uint_as_float(w[e])));
+      } else {  // the cut of the largest float is the largest bf16
+        const uint32_t lo = __float_as_uint(logit(__uint_as_float(w[e] << 16))), hi = __float_as_uint(logit(__uint_as_float(w[e] & 0xffff0000u)));
+        w[e] = lo >> 16 | (hi & 0xffff0000u);
+      }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ __forceinline__ uint4 run(int q) const { return q < n_lds ? lds[q] : load(q); }
+  // f(logit, number in the run)
+  template <typename F>
+  static __device__ __forceinline__ void tokens(const uint4& v, F&& f) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if constexpr (VEC == 4) {
-        const float z = __uint_as_float(w[e]);
-        f(FIX ? logit(z) : z, q * 4 + e);
+        f(__uint_as_float(w[e]), e);
       } else {
-        const float a = __uint_as_float(w[e] << 16), b = __uint_as_float(w[e] & 0xffff0000u);
-        f(FIX ? logit(a) : a, q * 8 + 2 * e);
-        f(FIX ? logit(b) : b, q * 8 + 2 * e + 1);
+        f(__uint_as_float(w[e] << 16), 2 * e);
+        f(__uint_as_float(w[e] & 0xffff0000u), 2 * e + 1);
       }
     }
   }
-  // Every run once: f(fix, run, number), fix false where all logits are finite.  Four loads from memory are under way together.
-  template <bool FIX, typename F>
-  __device__ __forceinline__ void all(F& f) const {
-    constexpr std::integral_constant<bool, FIX> fix{};
-    for (int q = threadIdx.x; q < n_lds; q += NT) f(fix, lds[q], q);
-    for (int q0 = n_lds + threadIdx.x; q0 < n_vec; q0 += 4 * NT) {
-      uint4 v[4];
-#pragma unroll
-      for (int s = 0; s < 4; ++s) v[s] = q0 + s * NT < n_vec ? load(q0 + s * NT) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-        if (q0 + s * NT < n_vec) f(fix, v[s], q0 + s * NT);
-    }
-  }
+  // Every run once: f(run, number); tokens past the row's end are -inf.  The next run is asked for before this one's work, which stands here
+  // once: a pass of several copies of it does not fit the instruction cache.
   template <typename F>
   __device__ __forceinline__ void runs(F f) const {
-    if (odd) all<true>(f);
-    else all<false>(f);
+    int q = threadIdx.x;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (q < n_vec) v = run(q);
+#pragma unroll 1
+    while (q < n_vec) {
+      const int at = q;
+      uint4 now = v;
+      q += NT;
+      if (q < n_vec) v = run(q);
+      if (odd) now = mended(now);
+      f(now, at);
+    }
   }
-  // The same by tokens: f(logit, index); tokens past the row's end are -inf.
+  // The same by tokens: f(logit, index).
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
-    runs([&](auto fix, const uint4& v, int q) { tokens<decltype(fix)::value>(v, q, f); });
+    runs([&](const uint4& v, int q) { tokens(v, [&](float z, int e) { f(z, q * VEC + e); }); });
   }
   // The first pass: what LDS holds goes there; f as in all(), with the logits as they are.
   template <typename F>
@@ -136,21 +147,27 @@ struct Row {
       for (int s = 0; s < 8; ++s) {
         const int q = q0 + s * NT;
         if (q < n_lds) lds[q] = v[s];
-        if (q < n_vec) tokens<false>(v[s], q, f);
+        if (q < n_vec) tokens(v[s], f);
       }
     }
   }
 };
 
-// The listed tokens of a row.
+// All tokens of a row, or the listed ones.
 template <typename T>
-struct Listed {
+struct Tokens {
   const Row<T>& row;
   const unsigned* list;
   int n;
+  bool listed;
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
-    for (int e = threadIdx.x; e < n; e += NT) f(row.at((int)list[e]), (int)list[e]);
+    if (!listed) {
+      row.each(f);
+    } else {
+#pragma unroll 1
+      for (int e = threadIdx.x; e < n; e += NT) f(row.at((int)list[e]), (int)list[e]);
+    }
   }
 };
 
@@ -167,22 +184,27 @@ __device__ __forceinline__ u64 fixed(float w) { return (u64)(w * 17592186044416.
 __device__ __forceinline__ double bin_units(u64 w) { return (double)w * (1.0 / 1024.0); }
 constexpr double BIN_ONE = 17179869184.0;
 
-// In thread order: the sums of (n, w) before this thread's, and the sum of all w.
+// In the order of the first NS threads (whole waves; the others only come along): the sums of (n, w) before this thread's, and the sum of all w.
+// A step that every wave takes costs a SIMD four times what it costs one wave: bookkeeping is left to four of them.
+constexpr int NS = 256;
 __device__ __forceinline__ void block_scan(unsigned n, double w, unsigned& before_n, double& before_w, double& all_w, Shared& sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  before_n = 0, before_w = 0;
+  if (threadIdx.x < NS) {
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const unsigned pn = __shfl_up(n, d);
-    const double pw = __shfl_up(w, d);
-    if (lane >= d) n += pn, w += pw;
+    for (int d = 1; d < 64; d <<= 1) {
+      const unsigned pn = __shfl_up(n, d);
+      const double pw = __shfl_up(w, d);
+      if (lane >= d) n += pn, w += pw;
+    }
+    if (lane == 63) sh.part_n[wave] = n, sh.part_w[wave] = w;
+    before_n = __shfl_up(n, 1), before_w = __shfl_up(w, 1);
+    if (!lane) before_n = 0, before_w = 0;
   }
-  if (lane == 63) sh.part_n[wave] = n, sh.part_w[wave] = w;
-  before_n = __shfl_up(n, 1), before_w = __shfl_up(w, 1);
-  if (!lane) before_n = 0, before_w = 0;
   __syncthreads();
   all_w = 0;
 #pragma unroll
-  for (int i = 0; i < NT / 64; ++i) {
+  for (int i = 0; i < NS / 64; ++i) {
     if (i < wave) before_n += sh.part_n[i], before_w += sh.part_w[i];
     all_w += sh.part_w[i];
   }
@@ -217,11 +239,13 @@ __device__ __forceinline__ float edge(const Range& g, int bin, float zmax, float
 // sh.at: the first bin through which the sum of counts (by_mass: of weights) reaches k (the target; with p >= 0 that is p times the sum of all bins);
 // it stays -1 where none does.  sh.above_*: the sums before it; sh.here_n: its count; returns the target.
 __device__ __forceinline__ double find_bin(const Range& g, Shared& sh, float zmax, float inv, bool mass, bool by_mass, unsigned k, double target, float p, double& total) {
-  constexpr int PER = NB / NT;
-  const int b = PER * (int)threadIdx.x;
+  constexpr int PER = NB / NS;
+  const bool one = threadIdx.x < NS;
+  const int b = one ? PER * (int)threadIdx.x : 0;
   __syncthreads();
   unsigned n[PER], all_n = 0;
   double w[PER], all_w = 0;
+  if (one) {
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const u64 e = sh.bin[b + i];
@@ -232,6 +256,7 @@ __device__ __forceinline__ double find_bin(const Range& g, Shared& sh, float zma
                   ((double)exp2_hw(edge(g, b + i, zmax, inv)) * (BIN_ONE / 67108864.0)));
     all_n += n[i], all_w += w[i];
   }
+  }
   unsigned cn;
   double cw;
   const unsigned an = sh.above_n;
@@ -239,12 +264,14 @@ __device__ __forceinline__ double find_bin(const Range& g, Shared& sh, float zma
   block_scan(all_n, all_w, cn, cw, total, sh);
   if (p >= 0.f) target = (double)p * total;
   cn += an, cw += aw;
+  if (one) {
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const unsigned nn = cn + n[i];
     const double nw = cw + w[i];
     if (by_mass ? cw < target && nw >= target : cn < k && nn >= k) sh.at = b + i, sh.above_n = cn, sh.above_w = cw, sh.here_n = n[i];
     cn = nn, cw = nw;
+  }
   }
   __syncthreads();
   return target;
@@ -324,58 +351,49 @@ __device__ __forceinline__ void race(Best& b, float z, int i, float zmax, float 
   const float s = fmaxf((z - zmax) * inv - __builtin_amdgcn_logf(-__builtin_amdgcn_logf(fminf(u, 0.99999994f))), -FLT_MAX);
   if (s > b.s || (s == b.s && i < b.i)) b = {s, z, i};
 }
-// f(logit, index, uniform) for the tokens of every run of 16 bytes whose largest logit `maybe` takes.  The uniforms of four runs are
-// asked for together: a load each, behind its own test, would be waited for one by one.
-template <typename T, bool FIX, typename M, typename F>
-__device__ __forceinline__ void with_uniforms(const Row<T>& row, const float* u, M maybe, F f) {
-  constexpr int VEC = Row<T>::VEC;
-  const bool wide = (uintptr_t)u % 16 == 0;
-  for (int q0 = threadIdx.x; q0 < row.n_vec; q0 += 4 * NT) {
-    uint4 v[4];
-    float4 w[4][VEC / 4];
-    bool some[4];
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int q = q0 + s * NT;
-      some[s] = q < row.n_vec;
-      if (some[s]) v[s] = q < row.n_lds ? row.lds[q] : row.load(q);
-    }
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int first = (q0 + s * NT) * VEC;
-      float most = NEG_INF;
-      auto up = [&](float z, int) { most = fmaxf(most, z); };
-      if (some[s]) Row<T>::template tokens<FIX>(v[s], 0, up);
-      some[s] = some[s] && maybe(most);
-      if (some[s]) {
-        if (wide && first + VEC <= row.V) {
-#pragma unroll
-          for (int e = 0; e < VEC / 4; ++e) w[s][e] = *reinterpret_cast<const float4*>(u + first + 4 * e);
-        } else {
-          float x[VEC];
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) x[e] = u[min(first + e, row.V - 1)];
-#pragma unroll
-          for (int e = 0; e < VEC / 4; ++e) w[s][e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
-        }
-      }
-    }
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-      if (some[s]) {
-        const int first = (q0 + s * NT) * VEC;
-        auto one = [&](float z, int e) {
-          const float4 x = w[s][e >> 2];
-          f(z, first + e, (e & 3) == 0 ? x.x : (e & 3) == 1 ? x.y : (e & 3) == 2 ? x.z : x.w);
-        };
-        Row<T>::template tokens<FIX>(v[s], 0, one);
-      }
-  }
-}
+// f(logit, index, uniform) for the tokens of every run of 16 bytes whose largest logit `maybe` takes.  The next run's logits and uniforms are asked for
+// before this one's work.
 template <typename T, typename M, typename F>
 __device__ __forceinline__ void race_pass(const Row<T>& row, const float* u, M maybe, F f) {
-  if (row.odd) with_uniforms<T, true>(row, u, maybe, f);
-  else with_uniforms<T, false>(row, u, maybe, f);
+  constexpr int VEC = Row<T>::VEC;
+  const bool wide = (uintptr_t)u % 16 == 0;
+  struct Run { uint4 v; float4 u[VEC / 4]; bool some; };
+  auto fetch = [&](int q) {
+    Run r;
+    r.v = row.run(q);
+    if (row.odd) r.v = Row<T>::mended(r.v);
+    float most = NEG_INF;
+    Row<T>::tokens(r.v, [&](float z, int) { most = fmaxf(most, z); });
+    r.some = maybe(most);
+    if (r.some) {
+      const int first = q * VEC;
+      if (wide && first + VEC <= row.V) {
+#pragma unroll
+        for (int e = 0; e < VEC / 4; ++e) r.u[e] = *reinterpret_cast<const float4*>(u + first + 4 * e);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC / 4; ++e)
+          r.u[e] = make_float4(u[min(first + 4 * e, row.V - 1)], u[min(first + 4 * e + 1, row.V - 1)], u[min(first + 4 * e + 2, row.V - 1)],
+                               u[min(first + 4 * e + 3, row.V - 1)]);
+      }
+    }
+    return r;
+  };
+  int q = threadIdx.x;
+  Run next{};
+  if (q < row.n_vec) next = fetch(q);
+#pragma unroll 1
+  while (q < row.n_vec) {
+    const int first = q * VEC;
+    const Run now = next;
+    q += NT;
+    if (q < row.n_vec) next = fetch(q);
+    if (now.some)
+      Row<T>::tokens(now.v, [&](float z, int e) {
+        const float4 x = now.u[e >> 2];
+        f(z, first + e, (e & 3) == 0 ? x.x : (e & 3) == 1 ? x.y : (e & 3) == 2 ? x.z : x.w);
+      });
+  }
 }
 
 template <typename T>
@@ -419,123 +437,196 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
   float lse = 0.f;
   Best best = {NEG_INF, NEG_INF, 0x7fffffff};
   auto heavy = [&](float z) { return min_p <= 0.f || exp2_hw((z - zmax) * inv) >= min_p; };
+  const bool both = by_k && by_p;
+  const float p = fmaxf(top_p, 1e-30f);
+  constexpr int VEC = Row<T>::VEC;
+  // Tokens of run q to the list, one place asked for per wave (a place per lane, of one counter, costs each lane a turn).
+  auto list = [&](unsigned mask, int q) {
+    u64 hits[VEC];
+    unsigned before = 0, all = 0;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      hits[e] = __ballot(mask >> e & 1);
+      before = __builtin_amdgcn_mbcnt_hi((unsigned)(hits[e] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)hits[e], before));
+      all += (unsigned)__popcll(hits[e]);
+    }
+    const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&sh.n, (int)all);
+    at = __builtin_amdgcn_readfirstlane(at) + (int)before;
+    for (; mask; mask &= mask - 1, ++at)
+      if (at < LIST) sh.list[at] = (unsigned)(q * VEC + __ffs(mask) - 1);
+  };
+
+  Range range = {zmax, -FLT_MAX, fmaxf(zmax - DEPTH / inv, -FLT_MAX), false, 0, a.V, 0.f, 0, true};
+  range.begin();
+  double target = 0;
+  bool lse_left = want_lse, drawn = false, begun = false;
+  unsigned n = LIST + 1;  // tokens in the list that hold all that can be kept, or none such
   if (greedy) {
     row.each([&](float z, int i) {
       if (want_lse) lse += exp2_hw((z - zmax) * LOG2E);
       if (z == zmax && i < best.i) best = {0.f, z, i};
     });
-  } else if (!by_k && !by_p) {
-    if (want_lse) row.each([&](float z, int) { lse += exp2_hw((z - zmax) * LOG2E); });
-    race_pass(row, u, [&](float z) { return z > NEG_INF && heavy(z); }, [&](float z, int i, float x) {
-      if (z > NEG_INF && heavy(z)) race(best, z, i, zmax, inv, x);
+    drawn = true;
+  } else if (!by_k && !by_p && min_p <= 0.f) {
+    race_pass(row, u, [](float) { return true; }, [&](float z, int i, float x) {
+      if (want_lse) lse += exp2_hw((z - zmax) * LOG2E);
+      if (z > NEG_INF) race(best, z, i, zmax, inv, x);
     });
-  } else {
-    // the first round, over all tokens that can be drawn
-    Range range = {zmax, -FLT_MAX, fmaxf(zmax - DEPTH / inv, -FLT_MAX), false, 0, a.V, 0.f, 0, true};
-    range.begin();
-    const float step = inv / range.c;  // log2 of the weights of two edges
-    const bool lse_here = want_lse && !(by_p && inv == LOG2E);  // at temperature 1 it is the sum of all weights
-    auto count = [&](auto mass, auto more) {
-      row.runs([&](auto fix, const uint4& v, int q) {
-        auto one = [&](float z, int) {
-          const float d = zmax - z, t = d * range.c, bin = truncf(fminf(t, (float)(NB - 1)));
-          if constexpr (more) lse += exp2_hw(d * -LOG2E);
-          const unsigned w = mass ? (unsigned)fminf(exp2_hw(fmaf(bin - t, step, 26.f)), 134217728.f) : 0u;
-          if (!decltype(fix)::value || z > NEG_INF) atomicAdd(&sh.bin[(int)bin], (u64)w | 1ull << 45);
-        };
-        Row<T>::template tokens<decltype(fix)::value>(v, q, one);
+    drawn = true;
+  } else if (min_p > 0.f) {
+    // what min_p leaves is known beforehand, and mostly few: the other rules' ends matter only among those
+    const bool more = want_lse && inv != LOG2E;
+    float mass = 0.f;
+    row.runs([&](const uint4& v, int q) {
+      float w[VEC], most = 0.f;
+      Row<T>::tokens(v, [&](float z, int e) {
+        w[e] = exp2_hw((z - zmax) * inv);
+        mass += w[e];
+        most = fmaxf(most, w[e]);
       });
-    };
-    constexpr std::true_type yes{};
-    constexpr std::false_type no{};
-    if (by_p) {
-      if (lse_here) count(yes, yes);
-      else count(yes, no);
-    } else {
-      if (lse_here) count(no, yes);
-      else count(no, no);
+      if (more) Row<T>::tokens(v, [&](float z, int) { lse += exp2_hw((z - zmax) * LOG2E); });
+      if (__any(most >= min_p)) {
+        unsigned mask = 0;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) mask |= w[e] >= min_p ? 1u << e : 0u;
+        list(mask, q);
+      }
+    });
+    if (want_lse && !more) lse = mass;  // at temperature 1
+    lse_left = false;
+    mass = wave_sum(mass);
+    if ((tid & 63) == 0) sh.part_a[tid >> 6] = mass;
+    __syncthreads();
+    double total = 0;
+#pragma unroll
+    for (int i = 0; i < NT / 64; ++i) total += (double)sh.part_a[i];
+    target = p * (total * BIN_ONE);
+    n = sh.n;
+    if (n > LIST || (both && n < (unsigned)top_k)) {  // too many, or not all that top-p's sum is over
+      n = LIST + 1;
+      __syncthreads();
+      if (tid == 0) sh.n = 0;
     }
+  }
+  if (!drawn && n > LIST) {
+    // the first round, over all tokens that can be drawn
+    const float step = inv / range.c;  // log2 of the weights of two edges
+    const bool lse_here = lse_left && !(by_p && inv == LOG2E);  // at temperature 1 it is the sum of all weights
+    row.runs([&](const uint4& v, int) {
+      Row<T>::tokens(v, [&](float z, int) {
+        const float d = zmax - z, t = d * range.c, bin = truncf(fminf(t, (float)(NB - 1)));
+        const unsigned w = by_p ? (unsigned)fminf(exp2_hw(fmaf(bin - t, step, 26.f)), 134217728.f) : 0u;
+        atomicAdd(&sh.bin[(int)bin], (u64)(z > NEG_INF ? 1u << 13 : 0u) << 32 | w);
+      });
+      if (lse_here) Row<T>::tokens(v, [&](float z, int) { lse += exp2_hw((z - zmax) * LOG2E); });
+    });
     // both rules end at or before where the first one does: the k-th token, or without top-k the share of all mass
-    const bool both = by_k && by_p;
-    const float p = fmaxf(top_p, 1e-30f);
     double all_w;
-    double target = find_bin(range, sh, zmax, inv, by_p, !by_k, (unsigned)top_k, 0, by_k ? -1.f : p, all_w);
-    if (want_lse && !lse_here && tid == 0) lse = (float)(all_w * (1.0 / BIN_ONE));
-    const unsigned n = sh.at < 0 ? LIST + 1 : sh.above_n + sh.here_n;
-    auto rest = [&](const auto& tokens) {  // the rules that are left, over tokens that hold all that they can keep
-      Last t = find_last(tokens, sh, range, true, Last{-FLT_MAX, 0x7fffffff}, zmax, inv, !by_k, (unsigned)top_k, target, by_p);
-      if (!both) return t;
-      double total = sh.run_w;
-      if (sh.found_i < 0) {  // fewer than k tokens can be drawn: all of them are kept
-        double w = 0, x_w;
-        unsigned x_n;
-        tokens.each([&](float z, int) { w += (double)exp2_hw((z - zmax) * inv); });
-        __syncthreads();
-        block_scan(0, w * BIN_ONE, x_n, x_w, total, sh);
+    target = find_bin(range, sh, zmax, inv, by_p, !by_k, (unsigned)top_k, 0, by_k ? -1.f : p, all_w);
+    if (lse_left && !lse_here && tid == 0) lse = (float)(all_w * (1.0 / BIN_ONE));
+    begun = true;
+    if (sh.at >= 0) {
+      // to the list: all tokens up to the bin's end, where that many fit; otherwise those of the bin, where they do
+      n = sh.above_n + sh.here_n <= LIST ? sh.above_n + sh.here_n : LIST + 1;
+      const unsigned here = sh.here_n;
+      const float from = n <= LIST ? -1.f : (float)sh.at, to = sh.at == NB - 1 ? __builtin_inff() : (float)(sh.at + 1);
+      if (here <= LIST) {
+        row.runs([&](const uint4& v, int q) {
+          float most = NEG_INF;
+          Row<T>::tokens(v, [&](float z, int) { most = fmaxf(most, z); });
+          if (__any(most > NEG_INF && fminf((zmax - most) * range.c, FLT_MAX) < to)) {
+            unsigned mask = 0;
+            Row<T>::tokens(v, [&](float z, int e) {
+              const float at = fminf((zmax - z) * range.c, FLT_MAX);
+              mask |= z > NEG_INF && at >= from && at < to ? 1u << e : 0u;
+            });
+            list(mask, q);
+          }
+        });
       }
       __syncthreads();
-      if (tid == 0) sh.above_n = 0, sh.above_w = 0;
-      return find_last(tokens, sh, range, false, t, zmax, inv, true, 0, p * total, true);
-    };
-    if (n <= LIST) {
-      const float to = (float)(sh.at + 1);
-      const bool any = sh.at == NB - 1;
-      row.runs([&](auto fix, const uint4& v, int q) {
-        float most = NEG_INF;
-        auto up = [&](float z, int) { most = fmaxf(most, z); };
-        Row<T>::template tokens<decltype(fix)::value>(v, q, up);
-        if (most > NEG_INF && (any || (zmax - most) * range.c < to)) {
-          unsigned mask = 0;
-          auto one = [&](float z, int i) { mask |= z > NEG_INF && (any || (zmax - z) * range.c < to) ? 1u << (i % Row<T>::VEC) : 0u; };
-          Row<T>::template tokens<decltype(fix)::value>(v, 0, one);
-          int at = atomicAdd(&sh.n, __popc(mask));
-          for (; mask; mask &= mask - 1, ++at)
-            if (at < LIST) sh.list[at] = (unsigned)(q * Row<T>::VEC + __ffs(mask) - 1);
-        }
-      });
+    }
+  }
+  if (!drawn && n <= FEW) {  // a thread per token
+    Some& some = *reinterpret_cast<Some*>(sh.bin);
+    float z = NEG_INF, x = 0.f;
+    int i = 0, rank = 0;
+    u64 key = 0, own = 0, before = 0;
+    if (tid < (int)n) {
+      i = (int)sh.list[tid], z = row.at(i), x = u[i];
+      key = order_key(z, i), own = fixed(exp2_hw((z - zmax) * inv));
+    }
+    if (tid < FEW) some.key[tid] = key, some.w[tid] = 0;  // 0 behind the last one
+    __syncthreads();
+    if (tid < (int)n) {
+      for (unsigned q0 = 0; q0 < n; q0 += 16)  // sixteen reads under way together
+#pragma unroll
+        for (unsigned q = 0; q < 16; ++q) rank += some.key[q0 + q] > key;
+      some.w[rank] = own;
+    }
+    if (by_p) {  // weights in order, then their sums, by one wave
       __syncthreads();
-      if (n <= FEW) {
-        Some& some = *reinterpret_cast<Some*>(sh.bin);
-        float z = NEG_INF, x = 0.f;
-        int i = 0, rank = 0;
-        u64 key = 0, own = 0, before = 0;
-        if (tid < (int)n) {
-          i = (int)sh.list[tid], z = row.at(i), x = u[i];
-          key = order_key(z, i), own = fixed(exp2_hw((z - zmax) * inv));
-        }
-        if (tid < FEW) some.key[tid] = key, some.w[tid] = own;  // 0 behind the last one
-        __syncthreads();
-        if (tid < (int)n) {
-          for (unsigned q0 = 0; q0 < n; q0 += 8)  // eight reads under way together
+      if (tid < 64) {
+        const u64 w0 = some.w[2 * tid], w1 = some.w[2 * tid + 1];
+        u64 sum = w0 + w1;
 #pragma unroll
-            for (unsigned q = 0; q < 8; ++q) {
-              const u64 other = some.key[q0 + q], w = some.w[q0 + q];
-              if (other > key) ++rank, before += w;
-            }
-          if (both && rank == top_k - 1) sh.run_w = bin_units(before + own);
+        for (int d = 1; d < 64; d <<= 1) {
+          const u64 up = __shfl_up(sum, d);
+          if (tid >= d) sum += up;
         }
-        if (both) {
+        some.key[2 * tid] = sum - w0 - w1, some.key[2 * tid + 1] = sum - w1;
+        if (both && (top_k - 1) >> 1 == tid) sh.run_w = bin_units((top_k & 1) ? sum - w1 : sum);
+      }
+      __syncthreads();
+      if (both) target = p * sh.run_w;
+      if (tid < (int)n) before = some.key[rank];
+    }
+    if (tid < (int)n && (!by_k || rank < top_k) && (!by_p || !rank || bin_units(before) < target) && heavy(z)) race(best, z, i, zmax, inv, x);
+  } else if (!drawn) {
+    // the rules one after the other, the first one over the list or the whole row (where its bin's tokens did not fit)
+    const bool listed = n <= LIST;
+    Last t = {-FLT_MAX, 0x7fffffff};
+    Tokens<T> tokens = {row, sh.list, (int)n, listed};
+    if (begun && !listed && sh.at >= 0 && sh.here_n <= LIST) tokens.n = (int)sh.here_n, tokens.listed = true;
+    const int rules = (int)by_k + (int)by_p;
+#pragma unroll 1
+    for (int rule = 0; rule < rules; ++rule) {
+      if (rule) {
+        tokens.n = (int)n, tokens.listed = listed;
+        double total = sh.run_w;
+        if (sh.found_i < 0) {  // fewer than k tokens can be drawn: all of them are kept
+          double w = 0, x_w;
+          unsigned x_n;
+          tokens.each([&](float z, int) { w += (double)exp2_hw((z - zmax) * inv); });
           __syncthreads();
-          target = p * sh.run_w;
+          double* const sums = reinterpret_cast<double*>(sh.bin);
+          sums[tid] = w;
+          __syncthreads();
+          for (int i = NS + tid; tid < NS && i < NT; i += NS) w += sums[i];
+          block_scan(0, w * BIN_ONE, x_n, x_w, total, sh);
         }
-        if (tid < (int)n && (!by_k || rank < top_k) && (!by_p || !rank || bin_units(before) < target) && heavy(z)) race(best, z, i, zmax, inv, x);
-      } else {
-        const Listed<T> listed = {row, sh.list, (int)n};
-        const Last t = rest(listed);
-        for (int e0 = tid; e0 < (int)n; e0 += 4 * NT) {  // four gathers under way together
-          int i[4];
-          float z[4], x[4];
+        target = p * total;
+        __syncthreads();
+        if (tid == 0) sh.above_n = 0, sh.above_w = 0;
+      }
+      t = find_last(tokens, sh, range, begun && !rule, t, zmax, inv, rule || !by_k, (unsigned)top_k, target, by_p);
+    }
+    if (listed) {
+#pragma unroll 1
+      for (int e0 = tid; e0 < (int)n; e0 += 4 * NT) {  // four gathers under way together
+        int i[4];
+        float z[4], x[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) i[e] = e0 + e * NT < (int)n ? (int)sh.list[e0 + e * NT] : -1;
+        for (int e = 0; e < 4; ++e) i[e] = e0 + e * NT < (int)n ? (int)sh.list[e0 + e * NT] : -1;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) z[e] = i[e] >= 0 ? row.at(i[e]) : NEG_INF, x[e] = i[e] >= 0 ? u[i[e]] : 0.f;
+        for (int e = 0; e < 4; ++e) z[e] = i[e] >= 0 ? row.at(i[e]) : NEG_INF, x[e] = i[e] >= 0 ? u[i[e]] : 0.f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (z[e] > NEG_INF && kept(t, z[e], i[e]) && heavy(z[e])) race(best, z[e], i[e], zmax, inv, x[e]);
-        }
+        for (int e = 0; e < 4; ++e)
+          if (z[e] > NEG_INF && kept(t, z[e], i[e]) && heavy(z[e])) race(best, z[e], i[e], zmax, inv, x[e]);
       }
     } else {
-      const Last t = rest(row);
       race_pass(row, u, [&](float z) { return z >= t.z; }, [&](float z, int i, float x) {
         if (z > NEG_INF && kept(t, z, i) && heavy(z)) race(best, z, i, zmax, inv, x);
       });
@@ -545,8 +636,10 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
     const Best o = {__shfl_xor(best.s, d), __shfl_xor(best.z, d), __shfl_xor(best.i, d)};
     if (o.s > best.s || (o.s == best.s && o.i < best.i)) best = o;
   };
+  if (__any(best.s > NEG_INF)) {
 #pragma unroll
-  for (int d = 32; d; d >>= 1) join(d);
+    for (int d = 32; d; d >>= 1) join(d);
+  }
   lse = wave_sum(lse);
   __syncthreads();
   if ((tid & 63) == 0) sh.part_a[tid >> 6] = best.s, sh.part_i[tid >> 6] = best.i, sh.part_z[tid >> 6] = best.z, sh.part_b[tid >> 6] = lse;
