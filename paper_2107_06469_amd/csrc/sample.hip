@@ -307,6 +307,7 @@ __device__ __forceinline__ Last find_last(const R& row, Shared& sh, Range g, boo
     if (bin < 0) return t;
     const unsigned n = sh.here_n;
     if (n <= CAP) {
+      if (tid < CAP && tid >= (int)n) some.key[tid] = 0, some.w[tid] = 0;
       row.each([&](float z, int i) {
         if (g.in(t, z, i) && g.bin_of(z, i) == bin) {
           const int at = atomicAdd(&sh.n, 1);
@@ -316,17 +317,18 @@ __device__ __forceinline__ Last find_last(const R& row, Shared& sh, Range g, boo
       __syncthreads();
       if (tid < (int)n) {
         const u64 key = some.key[tid], own = some.w[tid];
-        unsigned before = sh.above_n, last = 0;
+        unsigned rank = 0;
         u64 w = 0;
-#pragma unroll 4
-        for (unsigned q = 0; q < n; ++q) {
-          const u64 other = some.key[q], weight = some.w[q];
-          if (other > key) ++before, w += weight;
-          last += other < key;
-        }
+        for (unsigned q0 = 0; q0 < n; q0 += 8)  // eight reads under way together
+#pragma unroll
+          for (unsigned q = 0; q < 8; ++q) {
+            const u64 other = some.key[q0 + q], weight = some.w[q0 + q];
+            rank += other > key;
+            w += other > key ? weight : 0;
+          }
         // (the bin's own sum has reached the target, so its last token has)
         const double cw = sh.above_w + bin_units(w), nw = sh.above_w + bin_units(w + own);
-        if (by_mass ? (cw < target || before == sh.above_n) && (nw >= target || !last) : before == k - 1)
+        if (by_mass ? (cw < target || !rank) && (nw >= target || rank == n - 1) : sh.above_n + rank == k - 1)
           sh.found_z = key_logit(key), sh.found_i = key_index(key), sh.run_w = nw;
       }
       __syncthreads();
