@@ -5,8 +5,9 @@
 //     where s grew, the codes held become round(code * (s_before / s));  new codes are round(x' * (1 / s)), to nearest even.
 // Every product and sum of a value is rounded by itself (no contraction), so a code depends on nothing but the formula.
 // One workgroup has one page of one head of keys or values, or a run of query rows: new rows pass through registers once (maximum, then codes),
-// and no two workgroups touch one scale.  Bound by HBM for whole prompts, by the launch and three dependent loads (length, page, scale) for
-// single tokens.
+// and no two workgroups touch one scale.  Bound by HBM for whole prompts (eight of up to 2048 tokens, 32 heads of 128, e4m3: 469 MB in 106 us,
+// 4.4 TB/s where a copy reaches 5.1; 397 us when the rows were read once for the maximum and again for the codes), by the launch and three
+// dependent loads (length, page, scale) for single tokens (3.6 us for one sequence and for 2 x 64).
 #include <float.h>
 
 #include "kernels.h"
@@ -183,6 +184,7 @@ __global__ __launch_bounds__(NT) void append_kernel(const AppendArgs a) {
 template <int KIND, int ROT>
 void run_append(const AppendArgs& a, dim3 grid, int nt, int upt, hipStream_t s) {
   if (nt == 64) hipLaunchKernelGGL((append_kernel<KIND, ROT, 64, 1>), grid, dim3(64), 0, s, a);
+  else if (nt == 128) hipLaunchKernelGGL((append_kernel<KIND, ROT, 128, 1>), grid, dim3(128), 0, s, a);
   else if (upt == 1) hipLaunchKernelGGL((append_kernel<KIND, ROT, 256, 1>), grid, dim3(256), 0, s, a);
   else if (upt == 2) hipLaunchKernelGGL((append_kernel<KIND, ROT, 256, 2>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((append_kernel<KIND, ROT, 256, 4>), grid, dim3(256), 0, s, a);
@@ -237,13 +239,14 @@ const char* append_refusal(const AppendArgs& a) {
   return nullptr;
 }
 
-// One wave per page and head where that holds the new rows, 256 threads otherwise.
+// Threads per page and head: as many as it can have units of new rows, in powers of two, 256 with up to four units each beyond that.  Idle waves
+// cost: 301 tokens at most of 16 sequences in pages of 32 rows of 64 (128 units) take 12.5 us with 128 threads, 14.5 with 256.
 hipError_t launch_append(const AppendArgs& args, hipStream_t s) {
   AppendArgs a = args;
   const CacheArgs& c = a.c;
   if (a.rot == ROT_NONE) a.rot_dim = 0;
   const int upr = c.DH / 16, rows = c.max_q < c.page ? c.max_q : c.page;
-  const int nt = rows * upr <= 64 ? 64 : 256, upt = (rows * upr + nt - 1) / nt;
+  const int nt = rows * upr <= 64 ? 64 : rows * upr <= 128 ? 128 : 256, upt = (rows * upr + nt - 1) / nt;
   const int64_t pages = (c.max_q + c.page - 2) / c.page + 1;
   const int64_t cache_blocks = pages * 2 * c.HKV;
   const int64_t q_blocks = a.has_q ? ((int64_t)c.max_q * a.H * upr + nt - 1) / nt : 0;
