@@ -11,7 +11,11 @@
 //   O^T[d,i] += V^T P^T: the accumulators of two 16-key tiles are, in that order, the B operand (k index = accumulator row), and the A operand is,
 //     for d = W (l%16) + c (W = DH/16 bytes, one load), byte c of the 8 keys' words: one byte permutation brings two keys' codes together.
 // A page's scale multiplies scores (keys) or probabilities (values, in units of 2^-15 of the largest scale met so far: f16 then holds weights down
-// to 2^-39 of the largest).
+// to 2^-39 of the largest).  Maxima, sums, scores and accumulators are fp32.
+//
+// Bound by HBM where there are keys to read, 2 DH bytes each and head: 2 x 64 sequences of up to 2048 tokens over 8 heads of 128 (406 MB) in 75 us,
+// 5.4 TB/s, where the loads alone of this kernel take 70; 8 of up to 32768 (385 MB) in 71.  One sequence of 513 tokens takes 9, nearly all of it
+// latency: lengths and pages, codes, the join of the waves.
 #include <algorithm>
 #include <type_traits>
 
@@ -121,7 +125,9 @@ struct CacheAttnPlan {
   int waves;           // of a workgroup of cache_attn_kernel; 0: cache_prompt_kernel
 };
 
-// NW waves share a run of keys, 32 at a time in turn, each with its own maximum, sum and accumulators; they are joined through LDS.
+// NW waves share a run of keys, 32 at a time in turn, each with its own maximum, sum and accumulators; they are joined through LDS.  A tile of V
+// is read past the caches' order of use, one of K through it (its rows are taken by two loads each): the other way round, 8 sequences of 32768
+// tokens take 78..85 us (V cached) and 82 (K past it) instead of 77.
 // blockIdx: x sequence and key/value head, y run of keys and row tile, z model.
 template <int DH, int NW>
 constexpr int attn_lds() { return NW * 16 * (DH + 4) * 4 + NW * 16 * 8; }
@@ -376,10 +382,13 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(const CacheAttnArgs
 // chunk and transposing reads both spread over the banks): codes are widened once for all of a workgroup's rows on their way there.  The
 // next tile's codes are in registers while this one's products run; one barrier a tile.  v_mfma_f32_32x32x16_f16:
 //   S^T[t,i] = K Q^T (lane: query l%32; accumulator rows 8q + 4(l/32) + e),  O^T[d,i] += V^T P^T, P from the accumulators as they are, V^T by transposing
-//   LDS reads.  A
-// page's scale of the keys is in the factor of its scores, that of the values, in units of the window's largest one, in the exponent of its
-// weights (their own sum takes it back): neither costs an instruction a score.  Weights carry 2^7 besides, so that f16 holds small ones.
-// What a window of 512 pages is (id and scales) waits in LDS, too.
+//   LDS reads.
+// A page's scale of the keys is in the factor of its scores, that of the values, in units of the window's largest one, in the exponent of its
+// weights (their own sum takes it back): neither costs an instruction a score.  Weights are rounded to f16 (11 bits, against the 9 that the result
+// keeps) with a factor of 2^7, so that it holds them down to 2^-31 of the largest; a page whose values are 2^-n of the window's largest
+// loses n of that range, which is an error of 2^-31 of the largest value.  What a window of 512 pages is (id and scales) waits in LDS, too.
+// Bound by the vector unit (53 % of the cycles: exponentials, maxima, widening) beside the matrix cores (31 %), two waves a SIMD: 8 prompts of up to
+// 2048 tokens, 32 heads of 128, int8, causal: 138 GFLOP of visible pairs in 215 us, 640 TFLOP/s (the 16-row tiles above: 638 us).
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 __device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -732,7 +741,8 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
   }
 }
 
-// The runs' partial sums of one row and head, in ascending order: one wave each.  A lane has the maximum and sum of one run (64 at a time).
+// The runs' partial sums of one row and head, in ascending order: one wave each.  A lane has the maximum and sum of one run (64 at a time).  Rows of
+// no sequence (past q_ptr[B]) have no partial sums and are left alone.
 template <int DH>
 __global__ __launch_bounds__(64) void cache_attn_join_kernel(const CacheAttnArgs a, const CacheAttnPlan pl) {
   constexpr int E = DH / 64;
@@ -741,6 +751,7 @@ __global__ __launch_bounds__(64) void cache_attn_join_kernel(const CacheAttnArgs
   const int tok = (int)(i / a.H), head = (int)(i - (int64_t)tok * a.H);
   const float* po = static_cast<const float*>(a.ws[g]) + (size_t)i * pl.n_split * DH + lane * E;
   const float2* ml = reinterpret_cast<const float2*>(static_cast<const float*>(a.ws[g]) + (size_t)n * pl.n_split * DH) + (size_t)i * pl.n_split;
+  const bool mine = !a.c.q_ptr || (tok >= a.c.q_ptr[0] && tok < a.c.q_ptr[a.c.B]);
   float mm = NEG_BIG;
   for (int s0 = 0; s0 < pl.n_split; s0 += 64) mm = fmaxf(mm, s0 + lane < pl.n_split ? ml[s0 + lane].x : NEG_BIG);
   mm = wave_max(mm);
@@ -766,6 +777,7 @@ __global__ __launch_bounds__(64) void cache_attn_join_kernel(const CacheAttnArgs
       }
     }
   }
+  if (!mine) return;
   const float f = ll > 0.f ? 1.0f / ll : (ll == 0.f ? 0.f : ll);
   bf16_t* dst = a.o[g] + (size_t)tok * a.ld_o + (size_t)head * DH + lane * E;
   if (E == 2) *reinterpret_cast<uint32_t*>(dst) = pack_bf16(o[0] * f, o[E - 1] * f);
@@ -775,6 +787,17 @@ __global__ __launch_bounds__(64) void cache_attn_join_kernel(const CacheAttnArgs
 
 int floor_log2(int v) { return 31 - __builtin_clz((unsigned)v); }
 
+// Which kernel, with how many waves, and how many runs a sequence's keys are split into; from the host's bounds alone.  All figures in us, heads of 128,
+// int8, as (this choice | the other one).
+// Prompt kernel or 16-row tiles, by rows of a key/value head.  Up to 64 rows four 16-row tiles read no more than the caches give again (64 rows:
+// 13 | 21 for one sequence, 32 | 38 for 8 of 4096 tokens, 63 | 65 for 32); beyond, where the chip is full, one pass over the codes wins (96 rows: 40 |
+// 53 and 72 | 93, 256 rows: 71 | 114 and 100 | 201).  Few rows' tiles over few keys stay with the 16-row tiles, which are more workgroups (one sequence of 4096
+// tokens, 96 rows: 14 | 22, 256 rows: 17 | 24), until the keys are many (96 rows over 32768: 46 | 64).
+// Eight waves or four.  Up to 512 tiles, two for a CU, the eight are what keeps loads under way (8 sequences of 32768 tokens, 8 heads: 73 | 78; 32
+// of 4096: 42 | 46; 40 to 60 of 4096: 61..73 | 64..82); above, four join faster (72 of 4096: 93 with eight, 98 with four in one run, but 1024 tokens: 21 | 23).
+// Runs.  Few tiles: as many as fill the 256 CUs once, of 256 keys at least; where the heads do that already, one, until it is longer than 8192 keys.  Up
+// to 640 keys the second launch costs more than it saves (300 tokens: 9 | 11, 513: 9.8 | 11.3; 800: 11.6 in one, 10.9 split).  The prompt kernel's blocks
+// run two to a CU: 512 of them, of 256 keys at least (35 and 56 | 53 and 87 with 256 blocks of 512).
 CacheAttnPlan plan_of(const CacheArgs& c, int H) {
   CacheAttnPlan p{};
   p.page_log2 = floor_log2(c.page);

@@ -11,6 +11,10 @@
 // additions matters.  Usually at most 4096 tokens stand before the end of that bin: their indices go to a list, and what is left of the rules
 // and the draw look at nothing else.  Up to 128 of them are ranked directly; of more, or over the whole row, the bin is the next round's range
 // until 256 tokens at most are left in it (equal logits are told apart by histograms over their indices).
+// Bound by one CU's vector unit and LDS atomics for many rows (256 of 131072 in bf16, top-p and min-p: 33 us, 2.0 TB/s; 2 x 64 of 32000 in fp32,
+// mixed rules: 32), by a chain of some ten barriers for one (32000, top-k and top-p: 17).  A min_p is looked at before the rest, since it leaves few
+// tokens to the others: the wide rows take 142 us with the histogram first.  A row that is read again from memory instead of LDS costs the single
+// row 54 instead of 24 (both with the histograms of that time).
 #include <float.h>
 
 #include "kernels.h"
@@ -247,15 +251,15 @@ __device__ __forceinline__ double find_bin(const Range& g, Shared& sh, float zma
   double w[PER], all_w = 0;
   if (one) {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const u64 e = sh.bin[b + i];
-    n[i] = (unsigned)(e >> 45);
-    w[i] = 0;
-    if (mass && n[i])  // two conversions: the sum has 45 bits
-      w[i] = rint(((double)((unsigned)(e >> 32) & 0x1fffu) * 4294967296.0 + (double)(unsigned)e) *
-                  ((double)exp2_hw(edge(g, b + i, zmax, inv)) * (BIN_ONE / 67108864.0)));
-    all_n += n[i], all_w += w[i];
-  }
+    for (int i = 0; i < PER; ++i) {
+      const u64 e = sh.bin[b + i];
+      n[i] = (unsigned)(e >> 45);
+      w[i] = 0;
+      if (mass && n[i])  // two conversions: the sum has 45 bits
+        w[i] = rint(((double)((unsigned)(e >> 32) & 0x1fffu) * 4294967296.0 + (double)(unsigned)e) *
+                    ((double)exp2_hw(edge(g, b + i, zmax, inv)) * (BIN_ONE / 67108864.0)));
+      all_n += n[i], all_w += w[i];
+    }
   }
   unsigned cn;
   double cw;
@@ -266,12 +270,12 @@ __device__ __forceinline__ double find_bin(const Range& g, Shared& sh, float zma
   cn += an, cw += aw;
   if (one) {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const unsigned nn = cn + n[i];
-    const double nw = cw + w[i];
-    if (by_mass ? cw < target && nw >= target : cn < k && nn >= k) sh.at = b + i, sh.above_n = cn, sh.above_w = cw, sh.here_n = n[i];
-    cn = nn, cw = nw;
-  }
+    for (int i = 0; i < PER; ++i) {
+      const unsigned nn = cn + n[i];
+      const double nw = cw + w[i];
+      if (by_mass ? cw < target && nw >= target : cn < k && nn >= k) sh.at = b + i, sh.above_n = cn, sh.above_w = cw, sh.here_n = n[i];
+      cn = nn, cw = nw;
+    }
   }
   __syncthreads();
   return target;

@@ -333,6 +333,28 @@ def test_attention_rows_before_the_first_token_see_nothing(torch, ops):
 
 
 @pytest.mark.parametrize("n", [2, 150])
+@pytest.mark.parametrize("total", [400, 3000])
+def test_rows_of_no_sequence_are_left_alone(torch, ops, n, total):
+    """A call with room for more rows than q_ptr gives out (one captured for the most rows there may be): in one run of keys and in several."""
+    s = Setup(torch, ops, INT8, 1, 2, 64, 32, [n, 1], [total, total // 2], 22)
+    H, rows = 4, s.n_tok + 5
+    q = torch.randn(rows, H * 64, device="cuda").to(torch.bfloat16)
+    qkv = torch.randn(rows, (H + 4) * 64, device="cuda").to(torch.bfloat16)
+    call = dict(s.call, n_tok=rows)
+    which = {k: call[k] for k in ("n_tok", "max_q", "max_len")}
+    size = ops.hydra_op_cache_attention_ws_bytes(s.cache, H, **which)
+    assert (size > 0) == (total == 3000)
+    ws = [torch.full((size,), 0xff, dtype=torch.uint8, device="cuda")] if size else None
+    o, lse = torch.full_like(q, 7.0), torch.full((rows, H), 7.0, device="cuda")
+    ops.hydra_op_cache_attention(s.cache, s.lens, H, H * 64, H * 64, True, 0.125, [q], [o], [lse], ws=ws, **call)
+    ops.hydra_op_cache_append(s.cache, s.lens, H, (H + 4) * 64, H * 64, [qkv], [q], **call)
+    torch.cuda.synchronize()
+    assert (o[s.n_tok:] == 7.0).all() and (lse[s.n_tok:] == 7.0).all()
+    assert torch.isfinite(o[:s.n_tok]).all() and not (o[:s.n_tok] == 7.0).all(1).any()
+    assert torch.equal(q[:s.n_tok], qkv[:s.n_tok, :H * 64]) and not torch.equal(q[s.n_tok:], qkv[s.n_tok:, :H * 64])
+
+
+@pytest.mark.parametrize("n", [2, 150])
 @pytest.mark.parametrize("kind", [INT8, E4M3])
 def test_attention_of_pages_that_are_not_there(torch, ops, kind, n):
     s = Setup(torch, ops, kind, 1, 1, 64, 32, [n, n, n], [160, 300, 151], 18)
