@@ -6,15 +6,18 @@
 //     (In log2 throughout: a factor and a constant that all scores share change nothing.)
 //   T <= 0: the largest logit.  logprob = z_token - log sum_i exp z_i over all tokens, at temperature 1.
 //   A logit of -inf or NaN is never drawn, +inf counts as the largest float; without a token that can be drawn: -1 and -inf.
-// A row is one workgroup's, its first 127 KB wait in LDS between the passes.  A histogram over the range of logits finds where the count or the
+// A row is one workgroup's, its first 126 KB wait in LDS between the passes.  A histogram over the range of logits finds where the count or the
 // sum of w is reached: 2048 bins hold a count and the sum of w over the bin's largest possible w, in fixed point (2^-26), so that no order of
 // additions matters.  Usually at most 4096 tokens stand before the end of that bin: their indices go to a list, and what is left of the rules
 // and the draw look at nothing else.  Up to 128 of them are ranked directly; of more, or over the whole row, the bin is the next round's range
 // until 256 tokens at most are left in it (equal logits are told apart by histograms over their indices).
-// Bound by one CU's vector unit and LDS atomics for many rows (256 of 131072 in bf16, top-p and min-p: 33 us, 2.0 TB/s; 2 x 64 of 32000 in fp32,
-// mixed rules: 32), by a chain of some ten barriers for one (32000, top-k and top-p: 17).  A min_p is looked at before the rest, since it leaves few
-// tokens to the others: the wide rows take 142 us with the histogram first.  A row that is read again from memory instead of LDS costs the single
-// row 54 instead of 24 (both with the histograms of that time).
+// Where the list's tokens are known without the histogram it is left out: those that min_p leaves, and for a small top_k those at or above the top_k-th of
+// the threads' largest logits.
+// Bound by one CU's vector unit, each instruction a token being 2048 cycles of 131072 tokens, and LDS atomics, for many rows: 256 of 131072 in bf16
+// with top-p and min-p 34 us, 2.0 TB/s; 2 x 64 of 32000 in fp32 with mixed rules 34, of which a row with a top-k of 1500 and top-p takes 27.  A
+// single row of 32000 with a top-k of 50 and top-p takes 13, a chain of passes and barriers.  With the histogram for these too, the 256 rows take 142 and the single
+// one 17.  Rows that do not fit LDS are read again, through the caches.  A kept set larger than the list costs another pass, over the uniforms
+// too (131072 tokens, top-p 0.97 alone: 115 us).
 #include <float.h>
 
 #include "kernels.h"
@@ -24,7 +27,10 @@ namespace hydra {
 namespace {
 
 constexpr int NT = 1024, NB = 2048, CAP = 256, FEW = 128, LIST = 4096;
-constexpr int ROW_BYTES = 130048;  // of a row in LDS
+// Up to this top_k it cuts first: the list is then short enough to be ranked directly, mostly (larger ones take longer that way: 1500 with top-p 30 us
+// instead of 26).  Bins of the threads' largest logits that tell where.
+constexpr int SMALL_K = 96, NC = 256;
+constexpr int ROW_BYTES = 129024;  // of a row in LDS
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_INF = -__builtin_inff();
@@ -51,11 +57,12 @@ __device__ __forceinline__ int key_index(u64 k) { return (int)(0xffffffffu - (un
 struct Shared {
   u64 bin[NB];      // count << 45 | sum of w / (largest w of the bin), 2^-26
   unsigned list[LIST];
+  unsigned top[NC];  // threads by their largest logit
   float part_a[NT / 64], part_b[NT / 64], part_z[NT / 64];
   int part_i[NT / 64];
   unsigned part_n[NT / 64];
   double part_w[NT / 64];
-  int n, at, odd, found_i;
+  int n, runs, at, odd, found_i;
   unsigned above_n, here_n;
   double above_w, run_w;
   float found_z;
@@ -418,7 +425,8 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
   const int top_k = a.top_k[r];
   const bool greedy = !(temp > 0.f);
   clear(sh);
-  if (tid == 0) sh.n = 0, sh.odd = 0, sh.above_n = 0, sh.above_w = 0;
+  if (tid < NC) sh.top[tid] = 0;
+  if (tid == 0) sh.n = 0, sh.runs = 0, sh.odd = 0, sh.above_n = 0, sh.above_w = 0;
   float most = NEG_INF;
   bool odd = false;
   row.first([&](float z, int) {
@@ -427,6 +435,12 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
   });
   const float zmax = fminf(block_max(most, sh.part_a), FLT_MAX);
   if (odd) sh.odd = 1;
+  const float by = greedy ? 1.f : fminf(fmaxf(1.0f / temp, 1e-30f), 1e30f), inv = LOG2E * by;
+  const bool by_k = !greedy && top_k > 0 && top_k < a.V, by_p = !greedy && top_p < 1.f, small_k = by_k && top_k <= SMALL_K;
+  Range range = {zmax, -FLT_MAX, fmaxf(zmax - DEPTH / inv, -FLT_MAX), false, 0, a.V, 0.f, 0, true};
+  range.begin();
+  const float coarse = range.c * ((float)NC / NB);
+  if (small_k) atomicAdd(&sh.top[(int)fminf((zmax - fminf(most, FLT_MAX)) * coarse, (float)(NC - 1))], 1u);
   __syncthreads();
   row.odd = sh.odd;
   if (zmax == NEG_INF) {
@@ -436,9 +450,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
     }
     return;
   }
-  const float by = greedy ? 1.f : fminf(fmaxf(1.0f / temp, 1e-30f), 1e30f), inv = LOG2E * by;
   const float* u = a.u[g] + (size_t)r * a.ldu;
-  const bool by_k = !greedy && top_k > 0 && top_k < a.V, by_p = !greedy && top_p < 1.f;
   const bool want_lse = a.logprob[g] != nullptr;
   float lse = 0.f;
   Best best = {NEG_INF, NEG_INF, 0x7fffffff};
@@ -446,29 +458,52 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
   const bool both = by_k && by_p;
   const float p = fmaxf(top_p, 1e-30f);
   constexpr int VEC = Row<T>::VEC;
-  // Tokens of run q to the list, one place asked for per wave (a place per lane, of one counter, costs each lane a turn).
-  auto list = [&](unsigned mask, int q) {
-    u64 hits[VEC];
-    unsigned before = 0, all = 0;
+  // To the list, in two steps, in any order: the runs with some token that `maybe` belongs there (their numbers take the bins' place), then the
+  // tokens of those that do.  One place is asked for per wave (a place per lane, of one counter, costs each lane a turn); LIST runs at most.
+  unsigned* const run_list = reinterpret_cast<unsigned*>(sh.bin);
+  static_assert(LIST * sizeof(unsigned) <= sizeof(sh.bin), "the runs take the bins' place");
+  auto place = [&](u64 hits, int first) { return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(hits >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)hits, (unsigned)first)); };
+  auto places = [&](int& counter, int all) {
+    int first = 0;
+    if (place(~0ull, 0) == 0) first = atomicAdd(&counter, all);
+    return __builtin_amdgcn_readfirstlane(first);
+  };
+  auto list_run = [&](bool maybe, int q) {
+    const u64 hits = __ballot(maybe);
+    if (!hits) return;
+    const int at = place(hits, places(sh.runs, __popcll(hits)));
+    if (maybe && at < LIST) run_list[at] = (unsigned)q;
+  };
+  auto list_tokens = [&](auto in) {
+    __syncthreads();
+    const int n_runs = min(sh.runs, LIST);
+#pragma unroll 1
+    for (int r = tid; r < n_runs; r += NT) {
+      const int q = (int)run_list[r];
+      uint4 v = row.run(q);
+      if (row.odd) v = Row<T>::mended(v);
+      u64 hits[VEC];
+      bool is[VEC];
+      int all = 0;
+      Row<T>::tokens(v, [&](float z, int e) {
+        is[e] = in(z);
+        hits[e] = __ballot(is[e]), all += __popcll(hits[e]);
+      });
+      int first = places(sh.n, all);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      hits[e] = __ballot(mask >> e & 1);
-      before = __builtin_amdgcn_mbcnt_hi((unsigned)(hits[e] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)hits[e], before));
-      all += (unsigned)__popcll(hits[e]);
+      for (int e = 0; e < VEC; ++e) {
+        const int at = place(hits[e], first);
+        if (is[e] && at < LIST) sh.list[at] = (unsigned)(q * VEC + e);
+        first += __popcll(hits[e]);
+      }
     }
-    const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
-    int at = 0;
-    if (lane == 0) at = atomicAdd(&sh.n, (int)all);
-    at = __builtin_amdgcn_readfirstlane(at) + (int)before;
-    for (; mask; mask &= mask - 1, ++at)
-      if (at < LIST) sh.list[at] = (unsigned)(q * VEC + __ffs(mask) - 1);
+    __syncthreads();
   };
 
-  Range range = {zmax, -FLT_MAX, fmaxf(zmax - DEPTH / inv, -FLT_MAX), false, 0, a.V, 0.f, 0, true};
-  range.begin();
   double target = 0;
   bool lse_left = want_lse, drawn = false, begun = false;
   unsigned n = LIST + 1;  // tokens in the list that hold all that can be kept, or none such
+  float bins = (float)NB;  // of the first round's that matter
   if (greedy) {
     row.each([&](float z, int i) {
       if (want_lse) lse += exp2_hw((z - zmax) * LOG2E);
@@ -481,39 +516,56 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       if (z > NEG_INF) race(best, z, i, zmax, inv, x);
     });
     drawn = true;
-  } else if (min_p > 0.f) {
-    // what min_p leaves is known beforehand, and mostly few: the other rules' ends matter only among those
-    const bool more = want_lse && inv != LOG2E;
+  } else if (small_k || min_p > 0.f) {
+    // Tokens at or above a cut go to the list, in the pass that sums the weights.  What min_p leaves is known beforehand (with room for the
+    // rounding of w; it is looked at exactly in the end), and of the threads' largest logits, the top_k-th has top_k tokens at or above it.
+    float by_rank = __builtin_inff();
+    if (small_k) {
+      const uint4 c4 = reinterpret_cast<const uint4*>(sh.top)[tid & 63];
+      const int sum4 = (int)(c4.x + c4.y + c4.z + c4.w);
+      int upto = sum4;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int up = __shfl_up(upto, d);
+        if ((tid & 63) >= d) upto += up;
+      }
+      // the bin that reaches top_k, in the one lane whose bins do
+      const unsigned b0 = (unsigned)(upto - sum4) + c4.x, b1 = b0 + c4.y, b2 = b1 + c4.z, k = (unsigned)top_k;
+      const int at = 4 * (tid & 63) + (int)(b0 < k) + (int)(b1 < k) + (int)(b2 < k);
+      const int bin = __builtin_amdgcn_readlane(at, __ffsll(__ballot(upto >= top_k)) - 1);
+      if (bin < NC - 1) by_rank = (float)(bin + 1);
+    }
+    const float by_min = min_p > 0.f ? (1e-5f - 1.00001f * __builtin_amdgcn_logf(min_p)) / inv * coarse * 1.00001f : __builtin_inff();
+    const bool whole = by_min <= by_rank;  // the list gets all that can be kept
+    const float to = fminf(by_min, by_rank);
+    const float least = fmaxf(zmax - to / coarse * 1.0001f, -FLT_MAX);
+    const bool more = want_lse && !(by_p && inv == LOG2E);  // at temperature 1 it is the sum of all weights
     float mass = 0.f;
     row.runs([&](const uint4& v, int q) {
-      float w[VEC], most = 0.f;
-      Row<T>::tokens(v, [&](float z, int e) {
-        w[e] = exp2_hw((z - zmax) * inv);
-        mass += w[e];
-        most = fmaxf(most, w[e]);
-      });
+      float most = NEG_INF;
+      Row<T>::tokens(v, [&](float z, int) { most = fmaxf(most, z); });
+      if (by_p) Row<T>::tokens(v, [&](float z, int) { mass += exp2_hw((z - zmax) * inv); });
       if (more) Row<T>::tokens(v, [&](float z, int) { lse += exp2_hw((z - zmax) * LOG2E); });
-      if (__any(most >= min_p)) {
-        unsigned mask = 0;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) mask |= w[e] >= min_p ? 1u << e : 0u;
-        list(mask, q);
-      }
+      list_run(most >= least, q);
     });
-    if (want_lse && !more) lse = mass;  // at temperature 1
+    if (want_lse && !more) lse = mass;
     lse_left = false;
     mass = wave_sum(mass);
     if ((tid & 63) == 0) sh.part_a[tid >> 6] = mass;
-    __syncthreads();
+    list_tokens([&](float z) { return z >= least; });
     double total = 0;
 #pragma unroll
     for (int i = 0; i < NT / 64; ++i) total += (double)sh.part_a[i];
     target = p * (total * BIN_ONE);
-    n = sh.n;
-    if (n > LIST || (both && n < (unsigned)top_k)) {  // too many, or not all that top-p's sum is over
+    n = sh.runs > LIST ? LIST + 1 : sh.n;
+    if (n > LIST || !(n >= (unsigned)top_k || (whole && !both))) {  // too many, or not all that top_k keeps (or top_p's sum is over)
+      // where the cut holds all that the rules look at, what is below its bins need not be counted again
+      if (!by_k || n >= (unsigned)top_k) bins = fminf(bins, ceilf(to * ((float)NB / NC)) + 1.f);
       n = LIST + 1;
       __syncthreads();
-      if (tid == 0) sh.n = 0;
+      clear(sh);
+      if (tid == 0) sh.n = 0, sh.runs = 0;
+      __syncthreads();
     }
   }
   if (!drawn && n > LIST) {
@@ -524,13 +576,13 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       Row<T>::tokens(v, [&](float z, int) {
         const float d = zmax - z, t = d * range.c, bin = truncf(fminf(t, (float)(NB - 1)));
         const unsigned w = by_p ? (unsigned)fminf(exp2_hw(fmaf(bin - t, step, 26.f)), 134217728.f) : 0u;
-        atomicAdd(&sh.bin[(int)bin], (u64)(z > NEG_INF ? 1u << 13 : 0u) << 32 | w);
+        if (bin < bins) atomicAdd(&sh.bin[(int)bin], (u64)(z > NEG_INF ? 1u << 13 : 0u) << 32 | w);
       });
       if (lse_here) Row<T>::tokens(v, [&](float z, int) { lse += exp2_hw((z - zmax) * LOG2E); });
     });
     // both rules end at or before where the first one does: the k-th token, or without top-k the share of all mass
     double all_w;
-    target = find_bin(range, sh, zmax, inv, by_p, !by_k, (unsigned)top_k, 0, by_k ? -1.f : p, all_w);
+    target = find_bin(range, sh, zmax, inv, by_p, !by_k, (unsigned)top_k, target, by_k || bins < (float)NB ? -1.f : p, all_w);
     if (lse_left && !lse_here && tid == 0) lse = (float)(all_w * (1.0 / BIN_ONE));
     begun = true;
     if (sh.at >= 0) {
@@ -539,20 +591,23 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
       const unsigned here = sh.here_n;
       const float from = n <= LIST ? -1.f : (float)sh.at, to = sh.at == NB - 1 ? __builtin_inff() : (float)(sh.at + 1);
       if (here <= LIST) {
+        auto in = [&](float z) {
+          const float at = fminf((zmax - z) * range.c, FLT_MAX);
+          return z > NEG_INF && at >= from && at < to;
+        };
         row.runs([&](const uint4& v, int q) {
-          float most = NEG_INF;
-          Row<T>::tokens(v, [&](float z, int) { most = fmaxf(most, z); });
-          if (__any(most > NEG_INF && fminf((zmax - most) * range.c, FLT_MAX) < to)) {
-            unsigned mask = 0;
-            Row<T>::tokens(v, [&](float z, int e) {
-              const float at = fminf((zmax - z) * range.c, FLT_MAX);
-              mask |= z > NEG_INF && at >= from && at < to ? 1u << e : 0u;
-            });
-            list(mask, q);
+          bool some = false;
+          if (from < 0.f) {
+            float most = NEG_INF;
+            Row<T>::tokens(v, [&](float z, int) { most = fmaxf(most, z); });
+            some = in(most);
+          } else {
+            Row<T>::tokens(v, [&](float z, int) { some |= in(z); });
           }
+          list_run(some, q);
         });
+        list_tokens(in);
       }
-      __syncthreads();
     }
   }
   if (!drawn && n <= FEW) {  // a thread per token
