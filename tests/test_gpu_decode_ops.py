@@ -564,6 +564,25 @@ def test_sample_keeps_few_and_many(torch, ops, V, dtype, p):
     assert told >= len(ks)
 
 
+@pytest.mark.parametrize("V", [90, 4097, 32003, 131072])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("order", ["any", "falling", "steps"])
+def test_sample_cuts_that_hold_few_and_too_many(torch, ops, V, dtype, order):
+    """min_p that leaves one token to nearly all, small top_k, both: logits in any order, falling with the index, and in steps of equal ones."""
+    r = np.random.default_rng(V)
+    rules = [(k, p, m) for k in (0, 1, 40, 96, 97, 3000) for p, m in ((1.0, 0.3), (0.95, 0.01), (0.97, 1e-4), (0.5, 1e-7), (0.9, 0.0))]
+    k, p, m = (list(x) for x in zip(*rules))
+    z = logits(r, len(rules), V, "ranked").astype(np.float32)
+    if order != "any":
+        z = -np.sort(-z, axis=1)
+    if order == "steps":
+        z = np.round(z * 2) / 2
+    u = r.random((len(rules), V), dtype=np.float32)
+    t = [1.3 if i % 2 else 0.8 for i in range(len(rules))]
+    told = check_sample(torch, ops, [z, z * 0.05], [u, u], t, k, p, m, dtype, pad=V % 3)
+    assert told >= len(rules)
+
+
 @pytest.mark.parametrize("V", [500, 20000, 40000])
 def test_sample_of_equal_logits(torch, ops, V):
     """Ties at the edge of the kept: the lower index stays."""
