@@ -120,9 +120,10 @@ __device__ __forceinline__ float lane_float(float v, int lane) { return __uint_a
 
 struct CacheAttnPlan {
   int n_split, chunk;  // runs of keys, keys in one (a multiple of 128)
-  int n_rt;            // 16-row tiles, or 128-row blocks, of the sequence with the most rows
+  int n_rt;            // 16-row tiles, or the prompt kernel's blocks, of the sequence with the most rows
   int page_log2;
-  int waves;           // of a workgroup of cache_attn_kernel; 0: cache_prompt_kernel
+  int waves;           // of a workgroup
+  bool prompt;         // cache_prompt_kernel, 32 rows a wave; else cache_attn_kernel
 };
 
 // NW waves share a run of keys, 32 at a time in turn, each with its own maximum, sum and accumulators; they are joined through LDS.  A tile of V
@@ -798,17 +799,24 @@ int floor_log2(int v) { return 31 - __builtin_clz((unsigned)v); }
 // Runs.  Few tiles: as many as fill the 256 CUs once, of 256 keys at least; where the heads do that already, one, until it is longer than 8192 keys.  Up
 // to 640 keys the second launch costs more than it saves (300 tokens: 9 | 11, 513: 9.8 | 11.3; 800: 11.6 in one, 10.9 split).  The prompt kernel's blocks
 // run two to a CU: 512 of them, of 256 keys at least (35 and 56 | 53 and 87 with 256 blocks of 512).
+// Rows of a prompt block, heads of 128.  Eight waves widen a tile for 256 rows, not 128, but have a CU to themselves, and where the keys are those of the rows
+// a block's first waves wait for its last.  Worth it for few rows behind many keys (512 tokens behind 30000, four heads sharing: 260 | 283, behind
+// 7000, none sharing: 84 | 90), level for 4 times the keys (227 | 228), not for whole prompts (8 of 2048, four heads sharing: 275 | 292).
 CacheAttnPlan plan_of(const CacheArgs& c, int H) {
   CacheAttnPlan p{};
   p.page_log2 = floor_log2(c.page);
   const int64_t rows = (int64_t)c.max_q * (H / c.HKV), len = c.max_len;
   const int64_t heads = (int64_t)c.G * c.B * c.HKV, tiles = heads * ((rows + 15) / 16);
-  p.waves = rows > 64 && (tiles > 256 || len > 8192) ? 0 : tiles <= 512 ? 8 : 4;
-  p.n_rt = (int)((rows + (p.waves ? 15 : 127)) / (p.waves ? 16 : 128));
+  p.prompt = rows > 64 && (tiles > 256 || len > 8192);
+  if (p.prompt) p.waves = c.DH == 128 && rows >= 256 && len >= 8 * (int64_t)c.max_q ? 8 : 4;
+  else p.waves = tiles <= 512 ? 8 : 4;
+  const int64_t per = p.prompt ? p.waves * 32 : 16;
+  p.n_rt = (int)((rows + per - 1) / per);
   const int64_t base = heads * p.n_rt;
   int64_t n;
-  if (!p.waves) {
-    n = std::min((512 + base - 1) / base, (len + 255) / 256);
+  if (p.prompt) {
+    const int64_t blocks = p.waves == 8 ? 256 : 512;
+    n = std::min((blocks + base - 1) / base, (len + 255) / 256);
   } else {
     n = len <= 640 ? 1 : std::min(std::max(256 / base, (len + 8191) / 8192), (len + 255) / 256);
   }
@@ -819,8 +827,18 @@ CacheAttnPlan plan_of(const CacheArgs& c, int H) {
 
 template <int KIND, int DH>
 hipError_t run_attn(const CacheAttnArgs& a, const CacheAttnPlan& p, dim3 grid, hipStream_t s) {
-  if (!p.waves && p.page_log2 >= 6) hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH, 4, true>), grid, dim3(256), prompt_lds<DH>(), s, a, p);
-  else if (!p.waves) hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH, 4, false>), grid, dim3(256), prompt_lds<DH>(), s, a, p);
+  if (p.prompt) {
+    const bool big = p.page_log2 >= 6;
+    if constexpr (DH == 128) {
+      if (p.waves == 8) {
+        if (big) hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH, 8, true>), grid, dim3(512), prompt_lds<DH>(), s, a, p);
+        else hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH, 8, false>), grid, dim3(512), prompt_lds<DH>(), s, a, p);
+        return hipGetLastError();
+      }
+    }
+    if (big) hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH, 4, true>), grid, dim3(256), prompt_lds<DH>(), s, a, p);
+    else hipLaunchKernelGGL((cache_prompt_kernel<KIND, DH, 4, false>), grid, dim3(256), prompt_lds<DH>(), s, a, p);
+  }
   else if (p.waves == 4) hipLaunchKernelGGL((cache_attn_kernel<KIND, DH, 4>), grid, dim3(256), (attn_lds<DH, 4>()), s, a, p);
   else hipLaunchKernelGGL((cache_attn_kernel<KIND, DH, 8>), grid, dim3(512), (attn_lds<DH, 8>()), s, a, p);
   return hipGetLastError();
@@ -829,6 +847,12 @@ template <int KIND, int DH>
 hipError_t attn_init_kind() {
   hipError_t e = hipFuncSetAttribute((const void*)cache_attn_kernel<KIND, DH, 8>, hipFuncAttributeMaxDynamicSharedMemorySize, attn_lds<DH, 8>());
   if (e != hipSuccess) return e;
+  if constexpr (DH == 128) {
+    e = hipFuncSetAttribute((const void*)cache_prompt_kernel<KIND, DH, 8, false>, hipFuncAttributeMaxDynamicSharedMemorySize, prompt_lds<DH>());
+    if (e != hipSuccess) return e;
+    e = hipFuncSetAttribute((const void*)cache_prompt_kernel<KIND, DH, 8, true>, hipFuncAttributeMaxDynamicSharedMemorySize, prompt_lds<DH>());
+    if (e != hipSuccess) return e;
+  }
   e = hipFuncSetAttribute((const void*)cache_prompt_kernel<KIND, DH, 4, false>, hipFuncAttributeMaxDynamicSharedMemorySize, prompt_lds<DH>());
   if (e != hipSuccess) return e;
   return hipFuncSetAttribute((const void*)cache_prompt_kernel<KIND, DH, 4, true>, hipFuncAttributeMaxDynamicSharedMemorySize, prompt_lds<DH>());

@@ -314,6 +314,24 @@ def test_attention_of_prompts(torch, ops, kind, DH, page, H, HKV, new, total):
     check_attention(torch, ops, kind, 1, H, HKV, DH, page, new, total, True, 13)
 
 
+@pytest.mark.parametrize("kind", [INT8, E4M3])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("DH,page,H,HKV,new,total", [
+    (128, 64, 12, 12, [200, 1, 131], [200, 40, 150]), (64, 128, 12, 12, [200, 1, 131], [200, 40, 150]),   # blocks of 128 rows
+    (128, 16, 24, 6, [70, 65, 1], [700, 640, 130]), (128, 128, 32, 4, [40, 37, 0, 40], [400, 37, 5, 41]),  # of 256 rows, behind many keys
+    (64, 16, 24, 6, [210, 65], [700, 640])])
+def test_attention_of_prompts_by_blocks_of_rows(torch, ops, kind, causal, DH, page, H, HKV, new, total):
+    """As many rows as the kernel for prompts takes: more than 256 tiles of 16."""
+    check_attention(torch, ops, kind, 1, H, HKV, DH, page, new, total, causal, 23)
+
+
+@pytest.mark.parametrize("DH,H", [(64, 1), (128, 1), (128, 4)])
+def test_attention_of_prompts_behind_many_tokens(torch, ops, DH, H):
+    """Few blocks of rows and many keys: split, and joined."""
+    for page in (16, 64):
+        check_attention(torch, ops, INT8, 1, H, 1, DH, page, [70, 66], [8300, 100], True, 24)
+
+
 @pytest.mark.parametrize("one", [True, False])
 def test_attention_of_long_sequences(torch, ops, one):
     check_attention(torch, ops, E4M3, 1, 2, 1, 64, 16, [1, 1] if one else [1, 3], [9000, 4097], True, 14, one=one)
