@@ -338,6 +338,7 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t s);
 // ---- drawing tokens (sample.hip) -----------------------------------------------------------------------------------
 struct SampleArgs {
   int dtype, rows, V, ldz, ldu, G;
+  int row_bytes, list;       // of a row in LDS, tokens of the list: the launcher's
   const float* temperature;  // [rows], shared by the group, like top_k, top_p and min_p
   const int32_t* top_k;
   const float* top_p;

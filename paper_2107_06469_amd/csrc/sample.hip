@@ -26,11 +26,13 @@
 namespace hydra {
 namespace {
 
-constexpr int NT = 1024, NB = 2048, CAP = 256, FEW = 128, LIST = 4096;
+constexpr int NT = 1024, NB = 2048, CAP = 256, FEW = 128;
 // Up to this top_k it cuts first: the list is then short enough to be ranked directly, mostly (larger ones take longer that way: 1500 with top-p 30 us
 // instead of 26).  Bins of the threads' largest logits that tell where.
 constexpr int SMALL_K = 96, NC = 256;
-constexpr int ROW_BYTES = 129024;  // of a row in LDS
+// A row's bytes and the listed tokens share LDS: a row that fits leaves room for 4096 tokens, of one that does not less waits there for 8192 (256 rows of 131072 in
+// bf16 at temperature 1.3, a min-p of 0.0008: 49 us, with 4096 and more of the row 92).
+constexpr int ROW_BYTES = 129024, LIST = 4096, WIDE_ROW_BYTES = ROW_BYTES - 4 * LIST, WIDE_LIST = 2 * LIST;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_INF = -__builtin_inff();
@@ -56,7 +58,6 @@ __device__ __forceinline__ int key_index(u64 k) { return (int)(0xffffffffu - (un
 
 struct Shared {
   u64 bin[NB];      // count << 45 | sum of w / (largest w of the bin), 2^-26
-  unsigned list[LIST];
   unsigned top[NC];  // threads by their largest logit
   float part_a[NT / 64], part_b[NT / 64], part_z[NT / 64];
   int part_i[NT / 64];
@@ -419,7 +420,9 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
   row.p = static_cast<const T*>(a.z[g]) + (size_t)r * a.ldz;
   row.lds = row_lds;
   row.n_vec = (a.V + Row<T>::VEC - 1) / Row<T>::VEC;
-  row.n_lds = min(row.n_vec, ROW_BYTES / 16);
+  row.n_lds = min(row.n_vec, a.row_bytes / 16);
+  const int room = a.list;  // tokens of the list
+  unsigned* const the_list = reinterpret_cast<unsigned*>(row_lds + row.n_lds);
   row.wide = (uintptr_t)row.p % 16 == 0;
   const float temp = a.temperature[r], top_p = a.top_p[r], min_p = fminf(a.min_p[r], 1.f);
   const int top_k = a.top_k[r];
@@ -459,9 +462,9 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
   const float p = fmaxf(top_p, 1e-30f);
   constexpr int VEC = Row<T>::VEC;
   // To the list, in two steps, in any order: the runs with some token that `maybe` belongs there (their numbers take the bins' place), then the
-  // tokens of those that do.  One place is asked for per wave (a place per lane, of one counter, costs each lane a turn); LIST runs at most.
-  unsigned* const run_list = reinterpret_cast<unsigned*>(sh.bin);
-  static_assert(LIST * sizeof(unsigned) <= sizeof(sh.bin), "the runs take the bins' place");
+  // tokens of those that do.  One place is asked for per wave (a place per lane, of one counter, costs each lane a turn); as many runs at most as tokens.
+  uint16_t* const run_list = reinterpret_cast<uint16_t*>(sh.bin);
+  static_assert(WIDE_LIST * sizeof(uint16_t) <= sizeof(sh.bin), "the runs take the bins' place");
   auto place = [&](u64 hits, int first) { return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(hits >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)hits, (unsigned)first)); };
   auto places = [&](int& counter, int all) {
     int first = 0;
@@ -472,11 +475,11 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
     const u64 hits = __ballot(maybe);
     if (!hits) return;
     const int at = place(hits, places(sh.runs, __popcll(hits)));
-    if (maybe && at < LIST) run_list[at] = (unsigned)q;
+    if (maybe && at < room) run_list[at] = (uint16_t)q;
   };
   auto list_tokens = [&](auto in) {
     __syncthreads();
-    const int n_runs = min(sh.runs, LIST);
+    const int n_runs = min(sh.runs, room);
 #pragma unroll 1
     for (int r = tid; r < n_runs; r += NT) {
       const int q = (int)run_list[r];
@@ -493,7 +496,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         const int at = place(hits[e], first);
-        if (is[e] && at < LIST) sh.list[at] = (unsigned)(q * VEC + e);
+        if (is[e] && at < room) the_list[at] = (unsigned)(q * VEC + e);
         first += __popcll(hits[e]);
       }
     }
@@ -502,7 +505,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
 
   double target = 0;
   bool lse_left = want_lse, drawn = false, begun = false;
-  unsigned n = LIST + 1;  // tokens in the list that hold all that can be kept, or none such
+  unsigned n = room + 1;  // tokens in the list that hold all that can be kept, or none such
   float bins = (float)NB;  // of the first round's that matter
   if (greedy) {
     row.each([&](float z, int i) {
@@ -557,18 +560,18 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
 #pragma unroll
     for (int i = 0; i < NT / 64; ++i) total += (double)sh.part_a[i];
     target = p * (total * BIN_ONE);
-    n = sh.runs > LIST ? LIST + 1 : sh.n;
-    if (n > LIST || !(n >= (unsigned)top_k || (whole && !both))) {  // too many, or not all that top_k keeps (or top_p's sum is over)
+    n = sh.runs > room ? room + 1 : sh.n;
+    if (n > (unsigned)room || !(n >= (unsigned)top_k || (whole && !both))) {  // too many, or not all that top_k keeps (or top_p's sum is over)
       // where the cut holds all that the rules look at, what is below its bins need not be counted again
       if (!by_k || n >= (unsigned)top_k) bins = fminf(bins, ceilf(to * ((float)NB / NC)) + 1.f);
-      n = LIST + 1;
+      n = room + 1;
       __syncthreads();
       clear(sh);
       if (tid == 0) sh.n = 0, sh.runs = 0;
       __syncthreads();
     }
   }
-  if (!drawn && n > LIST) {
+  if (!drawn && n > (unsigned)room) {
     // the first round, over all tokens that can be drawn
     const float step = inv / range.c;  // log2 of the weights of two edges
     const bool lse_here = lse_left && !(by_p && inv == LOG2E);  // at temperature 1 it is the sum of all weights
@@ -587,10 +590,10 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
     begun = true;
     if (sh.at >= 0) {
       // to the list: all tokens up to the bin's end, where that many fit; otherwise those of the bin, where they do
-      n = sh.above_n + sh.here_n <= LIST ? sh.above_n + sh.here_n : LIST + 1;
+      n = sh.above_n + sh.here_n <= (unsigned)room ? sh.above_n + sh.here_n : room + 1;
       const unsigned here = sh.here_n;
-      const float from = n <= LIST ? -1.f : (float)sh.at, to = sh.at == NB - 1 ? __builtin_inff() : (float)(sh.at + 1);
-      if (here <= LIST) {
+      const float from = n <= (unsigned)room ? -1.f : (float)sh.at, to = sh.at == NB - 1 ? __builtin_inff() : (float)(sh.at + 1);
+      if (here <= (unsigned)room) {
         auto in = [&](float z) {
           const float at = fminf((zmax - z) * range.c, FLT_MAX);
           return z > NEG_INF && at >= from && at < to;
@@ -616,7 +619,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
     int i = 0, rank = 0;
     u64 key = 0, own = 0, before = 0;
     if (tid < (int)n) {
-      i = (int)sh.list[tid], z = row.at(i), x = u[i];
+      i = (int)the_list[tid], z = row.at(i), x = u[i];
       key = order_key(z, i), own = fixed(exp2_hw((z - zmax) * inv));
     }
     if (tid < FEW) some.key[tid] = key, some.w[tid] = 0;  // 0 behind the last one
@@ -647,10 +650,10 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
     if (tid < (int)n && (!by_k || rank < top_k) && (!by_p || !rank || bin_units(before) < target) && heavy(z)) race(best, z, i, zmax, inv, x);
   } else if (!drawn) {
     // the rules one after the other, the first one over the list or the whole row (where its bin's tokens did not fit)
-    const bool listed = n <= LIST;
+    const bool listed = n <= (unsigned)room;
     Last t = {-FLT_MAX, 0x7fffffff};
-    Tokens<T> tokens = {row, sh.list, (int)n, listed};
-    if (begun && !listed && sh.at >= 0 && sh.here_n <= LIST) tokens.n = (int)sh.here_n, tokens.listed = true;
+    Tokens<T> tokens = {row, the_list, (int)n, listed};
+    if (begun && !listed && sh.at >= 0 && sh.here_n <= (unsigned)room) tokens.n = (int)sh.here_n, tokens.listed = true;
     const int rules = (int)by_k + (int)by_p;
 #pragma unroll 1
     for (int rule = 0; rule < rules; ++rule) {
@@ -680,7 +683,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
         int i[4];
         float z[4], x[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) i[e] = e0 + e * NT < (int)n ? (int)sh.list[e0 + e * NT] : -1;
+        for (int e = 0; e < 4; ++e) i[e] = e0 + e * NT < (int)n ? (int)the_list[e0 + e * NT] : -1;
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[e] = i[e] >= 0 ? row.at(i[e]) : NEG_INF, x[e] = i[e] >= 0 ? u[i[e]] : 0.f;
 #pragma unroll
@@ -732,14 +735,18 @@ const char* sample_refusal(const SampleArgs& a) {
 }
 
 hipError_t sample_init() {
-  hipError_t e = hipFuncSetAttribute((const void*)sample_kernel<float>, hipFuncAttributeMaxDynamicSharedMemorySize, ROW_BYTES);
+  hipError_t e = hipFuncSetAttribute((const void*)sample_kernel<float>, hipFuncAttributeMaxDynamicSharedMemorySize, ROW_BYTES + 4 * LIST);
   if (e != hipSuccess) return e;
-  return hipFuncSetAttribute((const void*)sample_kernel<bf16_t>, hipFuncAttributeMaxDynamicSharedMemorySize, ROW_BYTES);
+  return hipFuncSetAttribute((const void*)sample_kernel<bf16_t>, hipFuncAttributeMaxDynamicSharedMemorySize, ROW_BYTES + 4 * LIST);
 }
 
-hipError_t launch_sample(const SampleArgs& a, hipStream_t s) {
+hipError_t launch_sample(const SampleArgs& args, hipStream_t s) {
+  SampleArgs a = args;
   const size_t esize = a.dtype == GEMM_F32 ? 4 : 2, row = ((size_t)a.V * esize + 15) / 16 * 16;
-  const unsigned lds = (unsigned)(row < ROW_BYTES ? row : ROW_BYTES);
+  const bool fits = row <= ROW_BYTES;
+  a.list = fits ? LIST : WIDE_LIST;
+  a.row_bytes = fits ? (int)row : WIDE_ROW_BYTES;
+  const unsigned lds = (unsigned)(a.row_bytes + 4 * a.list);
   const dim3 grid(a.rows, a.G);
   if (a.dtype == GEMM_F32) hipLaunchKernelGGL((sample_kernel<float>), grid, dim3(NT), lds, s, a);
   else hipLaunchKernelGGL((sample_kernel<bf16_t>), grid, dim3(NT), lds, s, a);
