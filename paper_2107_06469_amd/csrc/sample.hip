@@ -6,11 +6,11 @@
 //     (In log2 throughout: a factor and a constant that all scores share change nothing.)
 //   T <= 0: the largest logit.  logprob = z_token - log sum_i exp z_i over all tokens, at temperature 1.
 //   A logit of -inf or NaN is never drawn, +inf counts as the largest float; without a token that can be drawn: -1 and -inf.
-// A row is one workgroup's, its first 126 KB wait in LDS between the passes.  A histogram over the range of logits finds where the count or the
-// sum of w is reached: 2048 bins hold a count and the sum of w over the bin's largest possible w, in fixed point (2^-26), so that no order of
-// additions matters.  Usually at most 4096 tokens stand before the end of that bin: their indices go to a list, and what is left of the rules
-// and the draw look at nothing else.  Up to 128 of them are ranked directly; of more, or over the whole row, the bin is the next round's range
-// until 256 tokens at most are left in it (equal logits are told apart by histograms over their indices).
+// A row is one workgroup's; it waits in LDS between the passes, or as much of it as fits.  A histogram over the range of logits finds where the count or
+// the sum of w is reached: 2048 bins hold a count and the sum of w over the bin's largest possible w, in fixed point (2^-26), so that no order of
+// additions matters.  Usually at most 4096 tokens (8192 of a row that LDS does not hold) stand before the end of that bin: their indices go to a
+// list, and what is left of the rules and the draw look at nothing else.  Up to 128 of them are ranked directly; of more, or over the whole row, the
+// bin is the next round's range until 256 tokens at most are left in it (equal logits are told apart by histograms over their indices).
 // Where the list's tokens are known without the histogram it is left out: those that min_p leaves, and for a small top_k those at or above the top_k-th of
 // the threads' largest logits.
 // Bound by one CU's vector unit, each instruction a token being 2048 cycles of 131072 tokens, and LDS atomics, for many rows: 256 of 131072 in bf16
