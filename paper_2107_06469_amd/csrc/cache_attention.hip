@@ -801,13 +801,15 @@ int floor_log2(int v) { return 31 - __builtin_clz((unsigned)v); }
 // int8, as (this choice | the other one).
 // Prompt kernel or 16-row tiles, by rows of a key/value head.  Up to 64 rows four 16-row tiles read no more than the caches give again (64 rows:
 // 13 | 21 for one sequence, 32 | 38 for 8 of 4096 tokens, 63 | 65 for 32); beyond, where the chip is full, one pass over the codes wins (96 rows: 40 |
-// 53 and 72 | 93, 256 rows: 71 | 114 and 100 | 201).  Few rows' tiles over few keys stay with the 16-row tiles, which are more workgroups (one sequence of 4096
-// tokens, 96 rows: 14 | 22, 256 rows: 17 | 24), until the keys are many (96 rows over 32768: 46 | 64).
+// 53 and 72 | 93, 256 rows: 71 | 114 and 100 | 201).  Tiles that are few against the keys stay with the 16-row kernel, which has more workgroups (32 heads of one
+// sequence of 512 tokens: 16 to 21 | 21 to 27, 16 heads of 700: 20 | 25; but 1352 of four sequences, 2 heads, 1813 keys: 35 | 38, 12 heads of 64
+// short prompts: 13 | 31, 96 rows over 32768 keys: 46 | 64).
 // Eight waves or four.  Up to 512 tiles, two for a CU, the eight are what keeps loads under way (8 sequences of 32768 tokens, 8 heads: 73 | 78; 32
 // of 4096: 42 | 46; 40 to 60 of 4096: 61..73 | 64..82); above, four join faster (72 of 4096: 93 with eight, 98 with four in one run, but 1024 tokens: 21 | 23).
 // Runs.  Few tiles: as many as fill the 256 CUs once, of 256 keys at least; where the heads do that already, one, until it is longer than 8192 keys.  Up
 // to 640 keys the second launch costs more than it saves (300 tokens: 9 | 11, 513: 9.8 | 11.3; 800: 11.6 in one, 10.9 split).  The prompt kernel's blocks
-// run two to a CU: 512 of them, of 256 keys at least (35 and 56 | 53 and 87 with 256 blocks of 512).
+// run two to a CU: 512 of them, of 256 keys at least (35 and 56 | 53 and 87 with 256 blocks of 512); where
+// they fill the CUs once as it is, of 1024 at least (288 blocks: 300 keys 13 | 25 split, 1100 keys 39 | 48, but 4000 keys 102 split, 122 not).
 // Rows of a prompt block, heads of 128.  Eight waves widen a tile for 256 rows, not 128, but have a CU to themselves, and where the keys are those of the rows
 // a block's first waves wait for its last.  Worth it for few rows behind many keys (512 tokens behind 30000, four heads sharing: 260 | 283, behind
 // 7000, none sharing: 84 | 90), level for 4 times the keys (227 | 228), not for whole prompts (8 of 2048, four heads sharing: 275 | 292).
@@ -816,7 +818,7 @@ CacheAttnPlan plan_of(const CacheArgs& c, int H) {
   p.page_log2 = floor_log2(c.page);
   const int64_t rows = (int64_t)c.max_q * (H / c.HKV), len = c.max_len;
   const int64_t heads = (int64_t)c.G * c.B * c.HKV, tiles = heads * ((rows + 15) / 16);
-  p.prompt = rows > 64 && (tiles > 256 || len > 8192);
+  p.prompt = rows > 64 && (tiles > 1024 || tiles * len > 640 * 1024);
   if (p.prompt) p.waves = c.DH == 128 && rows >= 256 && len >= 8 * (int64_t)c.max_q ? 8 : 4;
   else p.waves = tiles <= 512 ? 8 : 4;
   const int64_t per = p.prompt ? p.waves * 32 : 16;
@@ -825,7 +827,7 @@ CacheAttnPlan plan_of(const CacheArgs& c, int H) {
   int64_t n;
   if (p.prompt) {
     const int64_t blocks = p.waves == 8 ? 256 : 512;
-    n = std::min((blocks + base - 1) / base, (len + 255) / 256);
+    n = base > blocks / 2 ? std::max(std::min((blocks + base - 1) / base, len / 1024), (int64_t)1) : std::min((blocks + base - 1) / base, (len + 255) / 256);
   } else {
     n = len <= 640 ? 1 : std::min(std::max(256 / base, (len + 8191) / 8192), (len + 255) / 256);
   }

@@ -325,6 +325,18 @@ def test_attention_of_prompts_by_blocks_of_rows(torch, ops, kind, causal, DH, pa
     check_attention(torch, ops, kind, 1, H, HKV, DH, page, new, total, causal, 23)
 
 
+@pytest.mark.parametrize("kind,causal", [(INT8, True), (E4M3, True), (INT8, False)])
+@pytest.mark.parametrize("DH,page", [(128, 16), (128, 64), (64, 32), (64, 128)])
+def test_attention_of_more_than_1024_tiles(torch, ops, kind, causal, DH, page):
+    check_attention(torch, ops, kind, 1, 32, 16, DH, page, [200, 1, 131], [230, 40, 131], causal, 25)
+
+
+@pytest.mark.parametrize("kind,page", [(INT8, 64), (E4M3, 16)])
+def test_attention_of_few_rows_behind_many_keys(torch, ops, kind, page):
+    """Blocks of 256 rows, split runs of keys, joined."""
+    check_attention(torch, ops, kind, 1, 4, 1, 128, page, [70], [38000], True, 26)
+
+
 @pytest.mark.parametrize("DH,H", [(64, 1), (128, 1), (128, 4)])
 def test_attention_of_prompts_behind_many_tokens(torch, ops, DH, H):
     """Few blocks of rows and many keys: split, and joined."""
