@@ -5,7 +5,7 @@
 //     where s grew, the codes held become round(code * (s_before / s));  new codes are round(x' * (1 / s)), to nearest even.
 // Every product and sum of a value is rounded by itself (no contraction), so a code depends on nothing but the formula.
 // One workgroup has one page of one head of keys or values, or a run of query rows: new rows pass through registers once (maximum, then codes),
-// and no two workgroups touch one scale.  Bound by HBM for whole prompts (eight of up to 2048 tokens, 32 heads of 128, e4m3: 469 MB in 106 us,
+// and no two workgroups touch one scale.  Bound by HBM for whole prompts (eight of up to 2048 tokens, 32 heads of 128, e4m3: 463 MB in 106 us,
 // 4.4 TB/s where a copy reaches 5.1; 397 us when the rows were read once for the maximum and again for the codes), by the launch and three
 // dependent loads (length, page, scale) for single tokens (3.6 us for one sequence and for 2 x 64).
 #include <float.h>
