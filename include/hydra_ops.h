@@ -221,7 +221,7 @@ size_t hydra_op_cache_attention_ws_bytes(const hydra_cache_desc* cache, int H);
  * whose sum of w reaches top_p times the sum over all of them (top_p >= 1: all, at least one token always); of those the tokens with w_i >= min_p
  * times the largest.  token_g[row] = argmax over the kept of z_i / temperature - log(-log u_i), which draws i with probability proportional to
  * w_i; temperature <= 0: the largest logit.  logprob_g[row] (table NULL: not wanted) = log softmax(z)[token], over all tokens at temperature 1.
- * Logits of -inf or NaN are never drawn, +inf counts as the largest fp32 number; a row without a token to draw gets -1 and -inf. */
+ * Logits of -inf or NaN are never drawn, +inf counts as the largest number of the logits' dtype; a row without a token to draw gets -1 and -inf. */
 int hydra_op_sample(int dtype, int rows, int V, int ldz, int ldu, int G, const void* const* logits, const float* const* u,
                     const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int32_t* const* token,
                     float* const* logprob, void* stream);

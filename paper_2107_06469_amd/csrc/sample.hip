@@ -5,7 +5,7 @@
 //   token = argmax over kept of z_i / T - log(-log u_i), the lowest index first: with u uniform, a draw with probabilities proportional to w_i.
 //     (In log2 throughout: a factor and a constant that all scores share change nothing.)
 //   T <= 0: the largest logit.  logprob = z_token - log sum_i exp z_i over all tokens, at temperature 1.
-//   A logit of -inf or NaN is never drawn, +inf counts as the largest float; without a token that can be drawn: -1 and -inf.
+//   A logit of -inf or NaN is never drawn, +inf counts as the largest number of the logits' type; without a token that can be drawn: -1 and -inf.
 // A row is one workgroup's; it waits in LDS between the passes, or as much of it as fits.  A histogram over the range of logits finds where the count or
 // the sum of w is reached: 2048 bins hold a count and the sum of w over the bin's largest possible w, in fixed point (2^-26), so that no order of
 // additions matters.  Usually at most 4096 tokens (8192 of a row that LDS does not hold) stand before the end of that bin: their indices go to a
@@ -43,7 +43,6 @@ struct Last { float z; int i; };  // the last kept token: kept are larger logits
 __device__ __forceinline__ bool kept(const Last& t, float z, int i) { return z > t.z || (z == t.z && i <= t.i); }
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float logit(float z) { return z == z ? fminf(z, FLT_MAX) : NEG_INF; }
 
 // an order of logits and indices as one of whole numbers: larger first
 __device__ __forceinline__ u64 order_key(float z, int i) {
@@ -76,6 +75,9 @@ static_assert(sizeof(Some) <= NB * sizeof(u64), "the ranked tokens take the bins
 template <typename T>
 struct Row {
   static constexpr int VEC = 16 / sizeof(T);
+  // What +inf counts as wherever a logit is looked at: the largest number of the type, so that a run of 16 bytes can hold it.
+  static constexpr float TOP = VEC == 4 ? FLT_MAX : 0x1.fep127f;
+  static __device__ __forceinline__ float logit(float z) { return z == z ? fminf(z, TOP) : NEG_INF; }
   const T* p;
   uint4* lds;
   int V, n_vec, n_lds;  // tokens; runs of VEC of them, the last one perhaps in part; runs in LDS
@@ -97,14 +99,14 @@ struct Row {
     if constexpr (VEC == 4) return logit(i < n_lds * VEC ? reinterpret_cast<const float*>(lds)[i] : p[i]);
     else return logit(__uint_as_float((uint32_t)(i < n_lds * VEC ? reinterpret_cast<const bf16_t*>(lds)[i] : p[i]) << 16));
   }
-  // NaN to -inf and +inf to the largest number, in a run
+  // NaN to -inf and +inf to TOP, in a run
   static __device__ __forceinline__ uint4 mended(uint4 v) {
     uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if constexpr (VEC == 4) {
         w[e] = __float_as_uint(logit(__uint_as_float(w[e])));
-      } else {  // the cut of the largest float is the largest bf16
+      } else {
         const uint32_t lo = __float_as_uint(logit(__uint_as_float(w[e] << 16))), hi = __float_as_uint(logit(__uint_as_float(w[e] & 0xffff0000u)));
         w[e] = lo >> 16 | (hi & 0xffff0000u);
       }
@@ -148,7 +150,7 @@ struct Row {
   __device__ __forceinline__ void each(F f) const {
     runs([&](const uint4& v, int q) { tokens(v, [&](float z, int e) { f(z, q * VEC + e); }); });
   }
-  // The first pass: what LDS holds goes there; f as in all(), with the logits as they are.
+  // The first pass: what LDS holds goes there; f(logit, number in the run), with the logits as they are.
   template <typename F>
   __device__ __forceinline__ void first(F f) const {
     for (int q0 = threadIdx.x; q0 < n_vec; q0 += 8 * NT) {
@@ -436,14 +438,14 @@ __global__ __launch_bounds__(NT) void sample_kernel(const SampleArgs a) {
     most = fmaxf(most, z);
     odd |= !(fabsf(z) <= FLT_MAX);
   });
-  const float zmax = fminf(block_max(most, sh.part_a), FLT_MAX);
+  const float zmax = fminf(block_max(most, sh.part_a), Row<T>::TOP);
   if (odd) sh.odd = 1;
   const float by = greedy ? 1.f : fminf(fmaxf(1.0f / temp, 1e-30f), 1e30f), inv = LOG2E * by;
   const bool by_k = !greedy && top_k > 0 && top_k < a.V, by_p = !greedy && top_p < 1.f, small_k = by_k && top_k <= SMALL_K;
   Range range = {zmax, -FLT_MAX, fmaxf(zmax - DEPTH / inv, -FLT_MAX), false, 0, a.V, 0.f, 0, true};
   range.begin();
   const float coarse = range.c * ((float)NC / NB);
-  if (small_k) atomicAdd(&sh.top[(int)fminf((zmax - fminf(most, FLT_MAX)) * coarse, (float)(NC - 1))], 1u);
+  if (small_k) atomicAdd(&sh.top[(int)fminf((zmax - fminf(most, Row<T>::TOP)) * coarse, (float)(NC - 1))], 1u);
   __syncthreads();
   row.odd = sh.odd;
   if (zmax == NEG_INF) {

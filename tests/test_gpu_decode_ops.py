@@ -667,3 +667,37 @@ def test_sample_frequencies(torch, ops):
     want = np.zeros(V)
     want[keep] = np.exp(z[0][keep] / 0.9) / np.exp(z[0][keep] / 0.9).sum()
     assert np.all(np.abs(got - want) <= 5 * np.sqrt(want * (1 - want) / n)), (got, want)
+
+
+# ---- cases of their own -----------------------------------------------------------------------------------------------
+
+BF16_TOP = float.fromhex("0x1.fep127")
+
+
+@pytest.mark.parametrize("V", [301, 3000, 70000])
+@pytest.mark.parametrize("k,p,m,t", [(0, 1.0, 0.0, 0.0), (0, 1.0, 0.05, 1.0), (0, 1.0, 0.0, 1.0), (10, 1.0, 0.0, 0.7), (200, 1.0, 0.0, 0.7), (200, 0.9, 0.0, 0.7),
+                                     (0, 0.9, 0.0, 1.2), (50, 0.8, 0.05, 1.0), (0, 0.9, 0.05, 1.0)], ids=str)
+def test_sample_of_16_bit_logits_that_are_no_numbers(torch, ops, V, k, p, m, t):
+    """+inf counts as the largest bf16 number in every form: alone, twice, and beside that number itself; NaN and -inf are never drawn."""
+    r = np.random.default_rng(V)
+    z = r.normal(size=(6, V)).astype(np.float32)
+    u = r.random((6, V), dtype=np.float32)
+    z[0, 77] = np.inf
+    z[1, 77], z[1, 99] = np.inf, np.inf
+    z[2, 20], z[2, 250] = np.inf, BF16_TOP
+    z[3, ::2], z[3, 101] = np.nan, np.inf
+    z[4, :], z[4, 9] = -np.inf, np.inf
+    z[5, ::3] = np.nan
+    z_dev = torch.from_numpy(z).cuda().to(torch.bfloat16)
+    full = lambda v, d: torch.full((6,), v, dtype=d, device="cuda")  # noqa: E731
+    token, logprob = full(-7, torch.int32), full(5.0, torch.float32)
+    ops.hydra_op_sample(ops.BF16, 6, V, V, V, [z_dev], [torch.from_numpy(u).cuda()], full(t, torch.float32), full(k, torch.int32), full(p, torch.float32),
+                        full(m, torch.float32), [token], [logprob])
+    got, got_lp = token.cpu().numpy(), logprob.cpu().numpy()
+    assert ((got >= 0) & (got < V)).all(), got
+    held = np.minimum(z_dev.float().cpu().numpy(), BF16_TOP)
+    for i in range(6):
+        tok, lp, gap, near = draw_64(held[i], u[i], t, k, np.float32(p), np.float32(m))
+        assert gap > 1e-4 and near > 2e-6 or i == 5                     # ordinary logits may be close; these are not
+        if gap > 1e-4 and near > 2e-6:
+            assert got[i] == tok and abs(got_lp[i] - lp) <= 2.0 ** -19 * (4 + abs(lp)), (i, got[i], tok, got_lp[i], lp)
