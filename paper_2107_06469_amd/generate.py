@@ -168,15 +168,20 @@ class Decoders:
         import torch
         positions = self.lens.to(torch.int64)
         self.lens.add_(1)
-        self._forward(self._single, list(self.tokens), positions)
+        # a model without a token to draw (its logits are no numbers) has -1 here and goes on from token 0: the embedding takes ids as they are
+        self._forward(self._single, list(self.tokens.clamp(0, self.arch["n_out"] - 1)), positions)
 
     def step(self, tokens=None):
-        """One token more per sequence: tokens [K, batch] (None: the ones in self.tokens); returns the next logits [K, batch, V]."""
+        """One token more per sequence: tokens [K, batch] of the vocabulary (looked at on the host; None: the ones in self.tokens, as they were drawn);
+        returns the next logits [K, batch, V]."""
         import torch
         if self._longest >= self.max_len:
             raise ValueError(f"a sequence has all of its {self.max_len} tokens")
         if tokens is not None:
-            self.tokens.copy_(torch.as_tensor(tokens))
+            tokens = torch.as_tensor(tokens)
+            if not (tokens.numel() and 0 <= int(tokens.min()) and int(tokens.max()) < self.arch["n_out"]):
+                raise ValueError(f"a token outside 0..{self.arch['n_out'] - 1}")
+            self.tokens.copy_(tokens)
         self._longest += 1
         if not self.graph:
             self._single_step()
@@ -193,7 +198,8 @@ class Decoders:
     def generate(self, prompts: Sequence[Sequence[int]], new_tokens: int, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0,
                  min_p: float = 0.0, seed: int = 0):
         """new_tokens drawn tokens per model and sequence and the log-probabilities that the model gave them: two arrays
-        [K, batch, new_tokens].  temperature 0 takes the largest logit."""
+        [K, batch, new_tokens].  temperature 0 takes the largest logit.  A model whose logits are no numbers has nothing to draw: -1 and -inf from there
+        on, the other models' tokens are what they would be without it."""
         import torch
         V, B = self.arch["n_out"], self.B
         if new_tokens < 1 or max(len(p) for p in prompts) + new_tokens - 1 > self.max_len:

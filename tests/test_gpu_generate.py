@@ -141,3 +141,15 @@ def test_refusals(G):
     d.prefill([list(range(16))])
     with pytest.raises(ValueError):
         d.step()
+
+
+@pytest.mark.parametrize("graph", [True, False])
+def test_a_model_whose_logits_are_no_numbers(G, graph):
+    """One diverged candidate of three: -1 and -inf for it, and the others' tokens as with a sound model in its place."""
+    arch, models = _models(1, 2, 3)
+    lost = [models[0], models[1][:-1] + [np.full_like(models[1][-1], np.nan)], models[2]]
+    (want, want_lp), (got, got_lp) = (G.Decoders(arch, m, len(PROMPT_LENGTHS), 48, page=16, graph=graph).generate(_prompts(), 7, top_k=20, seed=4)
+                                      for m in (models, lost))
+    assert (got[1] == -1).all() and np.isneginf(got_lp[1]).all()
+    assert np.array_equal(got[[0, 2]], want[[0, 2]]) and np.array_equal(got_lp[[0, 2]], want_lp[[0, 2]])
+    assert want.min() >= 0
