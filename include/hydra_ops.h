@@ -196,7 +196,7 @@ int hydra_op_cache_append(const hydra_cache_append_desc* d, void* stream);
 /* o_i = sum_t softmax_t(scale * q_i . k_t) v_t over the tokens t that the cache holds of the row's sequence, with causal those up to the
  * row's own position.  q_g [n_tok, ld_q] and o_g [n_tok, ld_o] bf16, H heads of DH columns; query head i reads key/value head i / (H/HKV).
  * lse_g (table NULL: not wanted) [n_tok, H] fp32: log-sum-exp of the scaled scores.  A row that sees no token gets o = 0 and lse = -inf, a row of no
- * sequence (past q_ptr[B]) is left alone.
+ * sequence (past q_ptr[B], or past the max_q that one may have) is left alone.
  * o_g may be q_g with the same leading dimension.  q, o 16-byte aligned, ld_q and ld_o multiples of 8.  What slots past a sequence's
  * length hold does not matter; codes of its tokens are numbers (hydra_op_cache_append stores no NaN).
  * ws_g: device scratch of hydra_op_cache_attention_ws_bytes bytes, 16-byte aligned, so that a sequence's tokens can be split over

@@ -751,8 +751,23 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
   }
 }
 
+// Whether some sequence of the call has row `tok`, as cache_seq says it (a wave's 64 lanes look at 64 places of q_ptr at a time; the last sequence that
+// begins at or before the row is the one that can).
+__device__ __forceinline__ bool row_of_call(const CacheArgs& c, int tok, int lane) {
+  if (!c.q_ptr) return true;
+  int lo = 0, hi = c.B;
+  while (true) {
+    const int step = (hi - lo + 63) >> 6, at = lo + lane * step;
+    const int before = __popcll(__ballot(at < hi && c.q_ptr[min(at, hi - 1)] <= tok));
+    if (!before) return false;
+    lo += (before - 1) * step, hi = min(lo + step, hi);
+    if (step == 1) break;
+  }
+  const CacheSeq sq = cache_seq(c, lo);
+  return tok >= sq.row0 && tok - sq.row0 < sq.n;
+}
 // The runs' partial sums of one row and head, in ascending order: one wave each.  A lane has the maximum and sum of one run (64 at a time).  Rows of
-// no sequence (past q_ptr[B]) have no partial sums and are left alone.
+// no sequence (past q_ptr[B], or past the max_q rows that one may have) have no partial sums and are left alone.
 template <int DH>
 __global__ __launch_bounds__(64) void cache_attn_join_kernel(const CacheAttnArgs a, const CacheAttnPlan pl) {
   constexpr int E = DH / 64;
@@ -761,7 +776,7 @@ __global__ __launch_bounds__(64) void cache_attn_join_kernel(const CacheAttnArgs
   const int tok = (int)(i / a.H), head = (int)(i - (int64_t)tok * a.H);
   const float* po = static_cast<const float*>(a.ws[g]) + (size_t)i * pl.n_split * DH + lane * E;
   const float2* ml = reinterpret_cast<const float2*>(static_cast<const float*>(a.ws[g]) + (size_t)n * pl.n_split * DH) + (size_t)i * pl.n_split;
-  const bool mine = !a.c.q_ptr || (tok >= a.c.q_ptr[0] && tok < a.c.q_ptr[a.c.B]);
+  if (!row_of_call(a.c, tok, lane)) return;
   float mm = NEG_BIG;
   for (int s0 = 0; s0 < pl.n_split; s0 += 64) mm = fmaxf(mm, s0 + lane < pl.n_split ? ml[s0 + lane].x : NEG_BIG);
   mm = wave_max(mm);
@@ -787,7 +802,6 @@ __global__ __launch_bounds__(64) void cache_attn_join_kernel(const CacheAttnArgs
       }
     }
   }
-  if (!mine) return;
   const float f = ll > 0.f ? 1.0f / ll : (ll == 0.f ? 0.f : ll);
   bf16_t* dst = a.o[g] + (size_t)tok * a.ld_o + (size_t)head * DH + lane * E;
   if (E == 2) *reinterpret_cast<uint32_t*>(dst) = pack_bf16(o[0] * f, o[E - 1] * f);

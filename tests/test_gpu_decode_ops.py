@@ -701,3 +701,22 @@ def test_sample_of_16_bit_logits_that_are_no_numbers(torch, ops, V, k, p, m, t):
         assert gap > 1e-4 and near > 2e-6 or i == 5                     # ordinary logits may be close; these are not
         if gap > 1e-4 and near > 2e-6:
             assert got[i] == tok and abs(got_lp[i] - lp) <= 2.0 ** -19 * (4 + abs(lp)), (i, got[i], tok, got_lp[i], lp)
+
+
+@pytest.mark.parametrize("total", [400, 3000])
+def test_rows_past_the_most_of_a_sequence_are_left_alone(torch, ops, total):
+    """A sequence with more rows in q_ptr than max_q allows: its first max_q rows are answered, the others left alone, in one run of keys and in several."""
+    s = Setup(torch, ops, INT8, 1, 2, 64, 32, [6, 0, 2, 70], [total, total // 2, total, total], 27)
+    H, most = 4, 3
+    q = torch.randn(s.n_tok, H * 64, device="cuda").to(torch.bfloat16)
+    call = dict(s.call, max_q=most)
+    size = ops.hydra_op_cache_attention_ws_bytes(s.cache, H, **{k: call[k] for k in ("n_tok", "max_q", "max_len")})
+    assert (size > 0) == (total == 3000)
+    ws = [torch.full((size,), 0xff, dtype=torch.uint8, device="cuda")] if size else None
+    o, lse = torch.full_like(q, 7.0), torch.full((s.n_tok, H), 7.0, device="cuda")
+    ops.hydra_op_cache_attention(s.cache, s.lens, H, H * 64, H * 64, True, 0.125, [q], [o], [lse], ws=ws, **call)
+    answered = torch.tensor([i for b, n in enumerate(s.new) for i in range(s.ptr[b], s.ptr[b] + min(n, most))], device="cuda")
+    rest = torch.ones(s.n_tok, dtype=torch.bool, device="cuda")
+    rest[answered] = False
+    assert (o[rest] == 7.0).all() and (lse[rest] == 7.0).all()
+    assert torch.isfinite(o[answered]).all() and not (o[answered] == 7.0).all(1).any()
