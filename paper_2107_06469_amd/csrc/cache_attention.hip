@@ -887,7 +887,8 @@ hipError_t attn_init_kind() {
 
 size_t cache_attn_ws_bytes(const CacheArgs& c, int H) {
   const CacheAttnPlan p = plan_of(c, H);
-  return p.n_split == 1 ? 0 : (size_t)c.n_tok * H * p.n_split * (c.DH + 2) * sizeof(float);
+  // (whole 16 bytes, so that scratch of several models lies in one allocation, each on its alignment)
+  return p.n_split == 1 ? 0 : ((size_t)c.n_tok * H * p.n_split * (c.DH + 2) * sizeof(float) + 15) / 16 * 16;
 }
 
 const char* cache_attn_sizes_refusal(const CacheArgs& c, int H) {

@@ -114,3 +114,27 @@ def test_cache_record_checks_its_tensors():
         a.update(bad)
         with pytest.raises(ValueError):
             ops.Cache(0, **a)
+
+
+@pytest.mark.parametrize("DH", [64, 128])
+def test_scratch_of_several_models_lies_in_one_allocation(DH):
+    """Odd rows, heads and runs: each model's part of one buffer is on the alignment that a call asks for."""
+    seen = set()
+    for H in (1, 2, 3, 5):
+        for n in (1, 3):
+            for length in (700, 1000, 1500, 9000):
+                d = cache(G=3, B=n, HKV=1, DH=DH, n_tok=n, max_pages=1000, max_len=length)[0]
+                size = ops._L().hydra_op_cache_attention_ws_bytes(ops._cache_desc(*d), H)
+                seen.add(size % 16)
+    assert seen == {0}
+
+
+def test_decoders_of_odd_sizes_cut_scratch_that_attention_takes():
+    """The scratch of generate.Decoders for one head and one sequence, split into three runs."""
+    from hydra_workloads import configs as C
+    from oracle import model as OM
+    from paper_2107_06469_amd import generate as G
+    arch = C.transformer_arch(C.KIND_DECODER, 1, 128, 1, 192, 301, 768, 0, C.DTYPE_BF16)
+    d = G.Decoders(arch, [OM.init_params(arch, 11, 0)] * 2, 1, 768, page=16, graph=False, device="cpu")
+    ws = d._single["ws"]
+    assert ws[0].numel() > 0 and (ws[1].data_ptr() - ws[0].data_ptr()) % 16 == 0
