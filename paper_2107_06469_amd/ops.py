@@ -217,24 +217,40 @@ def hydra_op_embed_bwd(dtype, V, S, S_table, B, d, ld, row_ptr, positions, dx, d
     _check(_L().hydra_op_embed_bwd(dtype, V, S, S_table, B, d, ld, len(dx), row_ptr.data_ptr(), positions.data_ptr(), *at, _stream()))
 
 
+# All tables of a call lie in one array: one that is too short would be read on into the next.
+def _one_per_model(G, *tables):
+    for t in tables:
+        if t is not None and len(t) != G:
+            raise ValueError(f"a table of {len(t)} tensors for {G} models")
+
+
+def _entries(t, n, dtype, name):
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{name} is contiguous {dtype} of at least {n} entries")
+
+
 class Cache:
     """One layer's paged cache of G models: pools of 8-bit codes k, v [n_pages, HKV, page, DH] (lists of G tensors), their scales k_scale, v_scale
     [n_pages, HKV] fp32 and the page table [B, max_pages] int32 that the group shares.  A record of tensors and their addresses: what the
     cache holds is in the tensors alone.  Pools may be slices along their first dimension's stride (several layers in one tensor)."""
 
     def __init__(self, kind, k, v, k_scale, v_scale, page_table):
+        import torch
+        self._int32 = torch.int32
         self.kind, self.k, self.v, self.k_scale, self.v_scale, self.page_table = kind, k, v, k_scale, v_scale, page_table
         n_pages, hkv, page, dh = k[0].shape
         stride = k[0].stride(0)
         for t in (*k, *v):
             if t.shape != k[0].shape or t.element_size() != 1 or t.stride() != (stride, page * dh, dh, 1):
                 raise ValueError("pools have one shape [n_pages, HKV, page, DH], one page stride and 1-byte codes, contiguous inside a page")
+        if n_pages > 1 and stride < hkv * page * dh:
+            raise ValueError("pages of a pool lie one behind the other")
         for t in (*k_scale, *v_scale):
-            if tuple(t.shape) != (n_pages, hkv) or t.element_size() != 4 or not t.is_contiguous():
+            if tuple(t.shape) != (n_pages, hkv) or t.dtype is not torch.float32 or not t.is_contiguous():
                 raise ValueError("scales are contiguous fp32 [n_pages, HKV]")
         if not len(k) == len(v) == len(k_scale) == len(v_scale):
             raise ValueError("k, v, k_scale and v_scale have one tensor per model")
-        if page_table.dim() != 2 or page_table.element_size() != 4 or not page_table.is_contiguous():
+        if page_table.dim() != 2 or page_table.dtype is not torch.int32 or not page_table.is_contiguous():
             raise ValueError("page_table is contiguous int32 [B, max_pages]")
         self.B, self.max_pages = page_table.shape
         self.HKV, self.page, self.DH, self.G = hkv, page, dh, len(k)
@@ -245,6 +261,10 @@ class Cache:
 
     def fields(self, lens=None, q_ptr=None, n_tok=None, max_q=1, max_len=None):
         """The fields of a call's hydra_cache_desc."""
+        if lens is not None and (lens.dtype is not self._int32 or lens.numel() < self.B or not lens.is_contiguous()):
+            raise ValueError(f"lens is contiguous int32 of at least {self.B} entries")
+        if q_ptr is not None and (q_ptr.dtype is not self._int32 or q_ptr.numel() <= self.B or not q_ptr.is_contiguous()):
+            raise ValueError(f"q_ptr is contiguous int32 of at least {self.B + 1} entries")
         return (*self._head, self.B if n_tok is None else n_tok, max_q, self.max_pages * self.page if max_len is None else max_len, self._stride,
                 self._table, 0 if lens is None else lens.data_ptr(), 0 if q_ptr is None else q_ptr.data_ptr(), *self._at)
 
@@ -256,6 +276,8 @@ _cache_desc, _append_desc, _attention_desc = (struct.Struct("11iN7P" + more).pac
 def hydra_op_cache_append(cache, lens, H, ld_qkv, ld_q, qkv, q=None, *, rot=ROT_NONE, rot_dim=0, cos_sin=None, q_ptr=None, n_tok=None, max_q=1,
                           max_len=None):
     """q=None leaves the queries alone; max_len=None: as many tokens as the page table has room for."""
+    if len(qkv) != cache.G or q is not None and len(q) != cache.G:
+        raise ValueError(f"qkv and q have one tensor for each of {cache.G} models")
     keep, tqkv, tq = _tabs(qkv, q)
     d = _append_desc(*cache.fields(lens, q_ptr, n_tok, max_q, max_len), H, ld_qkv, ld_q, rot, rot_dim, 0 if cos_sin is None else cos_sin.data_ptr(), tqkv,
                      tq or 0)
@@ -268,12 +290,19 @@ def hydra_op_cache_attention_ws_bytes(cache, H, *, n_tok=None, max_q=1, max_len=
 
 def hydra_op_cache_attention(cache, lens, H, ld_q, ld_o, causal, scale, q, o, lse=None, *, ws=None, q_ptr=None, n_tok=None, max_q=1, max_len=None):
     """ws: optional per-model scratch tensors (uint8, hydra_op_cache_attention_ws_bytes bytes) that allow splitting a sequence's tokens."""
+    _one_per_model(cache.G, q, o, lse, ws)
     keep, tq, to, tl, tw = _tabs(q, o, lse, ws)
     d = _attention_desc(*cache.fields(lens, q_ptr, n_tok, max_q, max_len), H, ld_q, ld_o, causal, scale, tq, to, tl or 0, tw or 0, _nbytes(ws))
     _check(_L().hydra_op_cache_attention(d, _stream()))
 
 
 def hydra_op_sample(dtype, rows, V, ldz, ldu, logits, u, temperature, top_k, top_p, min_p, token, logprob=None):
+    """temperature, top_p, min_p: fp32, top_k and every model's token: int32, of `rows` entries."""
+    import torch
+    _one_per_model(len(logits), u, token, logprob)
+    for name, t, kind in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                          ("min_p", min_p, torch.float32), *(("token", t, torch.int32) for t in token)):
+        _entries(t, rows, kind, name)
     keep, tz, tu, tt, tl = _tabs(logits, u, token, logprob)
     _check(_L().hydra_op_sample(dtype, rows, V, ldz, ldu, len(logits), tz, tu, temperature.data_ptr(), top_k.data_ptr(), top_p.data_ptr(),
                                 min_p.data_ptr(), tt, tl, _stream()))

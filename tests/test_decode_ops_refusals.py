@@ -138,3 +138,65 @@ def test_decoders_of_odd_sizes_cut_scratch_that_attention_takes():
     d = G.Decoders(arch, [OM.init_params(arch, 11, 0)] * 2, 1, 768, page=16, graph=False, device="cpu")
     ws = d._single["ws"]
     assert ws[0].numel() > 0 and (ws[1].data_ptr() - ws[0].data_ptr()) % 16 == 0
+
+
+# ---- what the bindings refuse by themselves: tables and arrays that the C side knows by their addresses alone -------------------------
+
+
+def two_models(**kw):
+    import torch
+    k = [torch.zeros((5, 2, 16, 64), dtype=torch.int8) for _ in range(2)]
+    a = dict(kind=0, k=k, v=k, k_scale=[torch.zeros((5, 2))] * 2, v_scale=[torch.zeros((5, 2))] * 2, page_table=torch.zeros((3, 2), dtype=torch.int32))
+    return ops.Cache(**{**a, **kw})
+
+
+def test_cache_record_checks_types_and_pages():
+    import torch
+    for bad in (dict(page_table=torch.zeros((3, 2))), dict(k_scale=[torch.zeros((5, 2), dtype=torch.int32)] * 2),
+                dict(v_scale=[torch.zeros((5, 2), dtype=torch.int32)] * 2),
+                dict(k=[torch.zeros((1, 2, 16, 64), dtype=torch.int8).expand(5, 2, 16, 64)] * 2,     # all pages in one place
+                     v=[torch.zeros((1, 2, 16, 64), dtype=torch.int8).expand(5, 2, 16, 64)] * 2)):
+        with pytest.raises(ValueError):
+            two_models(**bad)
+    one = [torch.zeros((1, 2, 16, 64), dtype=torch.int8)] * 2
+    two_models(k=one, v=one, k_scale=[torch.zeros((1, 2))] * 2, v_scale=[torch.zeros((1, 2))] * 2)
+
+
+@pytest.mark.parametrize("bad", ["qkv", "q", "o", "lse", "ws", "lens64", "lens_float", "lens_short", "lens_strided", "ptr64", "ptr_short"])
+@pytest.mark.parametrize("op", ["append", "attention"])
+def test_calls_are_checked_against_their_cache(op, bad, monkeypatch):
+    import torch
+    monkeypatch.setattr(ops, "_stream", lambda: 0)
+    c = two_models()
+    x = lambda n=2, w=384, t=torch.bfloat16: [torch.zeros((3, w), dtype=t) for _ in range(n)]  # noqa: E731
+    lens, ptr = torch.ones(3, dtype=torch.int32), torch.arange(4, dtype=torch.int32)
+    lens = {"lens64": lens.long(), "lens_float": lens.float(), "lens_short": lens[:2], "lens_strided": torch.ones(6, dtype=torch.int32)[::2]}.get(bad, lens)
+    ptr = {"ptr64": ptr.long(), "ptr_short": ptr[:3]}.get(bad, ptr)
+    n = lambda name: 1 if bad == name else 2  # noqa: E731
+    call = dict(q_ptr=ptr, n_tok=3, max_q=1)
+    if op == "append":
+        if bad in ("o", "lse", "ws"):
+            return
+        with pytest.raises(ValueError):
+            ops.hydra_op_cache_append(c, lens, 2, 384, 128, x(n("qkv")), x(n("q"), 128), **call)
+    else:
+        if bad == "qkv":
+            return
+        with pytest.raises(ValueError):
+            ops.hydra_op_cache_attention(c, lens, 2, 128, 128, True, 0.1, x(n("q"), 128), x(n("o"), 128), x(n("lse"), 2, torch.float32),
+                                         ws=x(n("ws"), 64, torch.uint8), **call)
+
+
+@pytest.mark.parametrize("bad", ["u", "token", "logprob", "top_k64", "temperature64", "top_p_int", "min_p_short", "token64", "top_k_strided"])
+def test_draws_are_checked(bad, monkeypatch):
+    import torch
+    monkeypatch.setattr(ops, "_stream", lambda: 0)
+    n = lambda name: 1 if bad == name else 2  # noqa: E731
+    z = [torch.zeros((3, 50))] * 2
+    rule = dict(t=torch.ones(3), k=torch.ones(3, dtype=torch.int32), p=torch.ones(3), m=torch.zeros(3))
+    rule.update({"top_k64": dict(k=torch.ones(3, dtype=torch.int64)), "temperature64": dict(t=torch.ones(3, dtype=torch.float64)),
+                 "top_p_int": dict(p=torch.ones(3, dtype=torch.int32)), "min_p_short": dict(m=torch.zeros(2)),
+                 "top_k_strided": dict(k=torch.ones(6, dtype=torch.int32)[::2])}.get(bad, {}))
+    token = [torch.zeros(3, dtype=torch.int64 if bad == "token64" else torch.int32)] * n("token")
+    with pytest.raises(ValueError):
+        ops.hydra_op_sample(ops.F32, 3, 50, 50, 50, z, z[:n("u")], *rule.values(), token, [torch.zeros(3)] * n("logprob"))
