@@ -198,7 +198,8 @@ int hydra_op_cache_append(const hydra_cache_append_desc* d, void* stream);
  * lse_g (table NULL: not wanted) [n_tok, H] fp32: log-sum-exp of the scaled scores.  A row that sees no token gets o = 0 and lse = -inf, a row of no
  * sequence (past q_ptr[B], or past the max_q that one may have) is left alone.
  * o_g may be q_g with the same leading dimension.  q, o 16-byte aligned, ld_q and ld_o multiples of 8.  What slots past a sequence's
- * length hold does not matter; codes of its tokens are numbers (hydra_op_cache_append stores no NaN).
+ * length hold does not matter; codes of its tokens are numbers (hydra_op_cache_append stores no NaN).  Scales of values below 2^-64 of a
+ * sequence's largest count as that.
  * ws_g: device scratch of hydra_op_cache_attention_ws_bytes bytes, 16-byte aligned, so that a sequence's tokens can be split over
  * workgroups whose results are joined in ascending order; it need not be initialised.  Without it (or with too little) nothing is split.
  * The size and the split depend on the descriptor's sizes and H alone. */

@@ -6,12 +6,14 @@
 //
 // Codes never leave registers between memory and the matrix cores.  Both products run on v_mfma_f32_16x16x32_f16: codes are exact in f16 (11
 // bits), p in f16 is rounded to 2^-12, finer than bf16 would, and a query row, bf16, is exact in f16 once the power of two of its largest
-// element is taken out (what is 2^-24 of that or less loses bits).
+// element is taken out (elements below 2^-17 of that are rounded to 2^-25 of it, half of what an fp32 sum with it may lose anyway).
 //   S^T[t,i] = K Q^T:  lane l supplies row t = l%16 of K, 16 bytes at a time as they lie in memory, and gets column i = l%16, rows 4(l/16) + e
 //   O^T[d,i] += V^T P^T: the accumulators of two 16-key tiles are, in that order, the B operand (k index = accumulator row), and the A operand is,
 //     for d = W (l%16) + c (W = DH/16 bytes, one load), byte c of the 8 keys' words: one byte permutation brings two keys' codes together.
-// A page's scale multiplies scores (keys) or probabilities (values, in units of 2^-15 of the largest scale met so far: f16 then holds weights down
-// to 2^-39 of the largest).  Maxima, sums, scores and accumulators are fp32.
+// A page's scale of keys multiplies its scores; that of its values, in units of the largest one met so far, is in the exponent of its weights, whose own sum
+// takes it back.  A row's maximum is that of what is in the exponents, so that f16, which holds weights down to 2^-39 of the largest, measures them by
+// what a page gives to the row, however small the values of the pages that the row looks at (down to 2^-64 of the largest; smaller scales
+// count as that).  Maxima, sums, scores and accumulators are fp32.
 //
 // Bound by HBM where there are keys to read, 2 DH bytes each and head: 2 x 64 sequences of up to 2048 tokens over 8 heads of 128 (406 MB) in 75 us,
 // 5.4 TB/s, where the loads alone of this kernel take 70; 8 of up to 32768 (385 MB) in 71.  One sequence of 513 tokens takes 9, nearly all of it
@@ -33,6 +35,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_BIG = -1.0e30f;
 constexpr float P_LOG2 = 15.f, P_ONE = 32768.f;  // a weight of 1 in f16
+constexpr float LEAST_UNITS = 0x1p-64f, SUM_LOG2 = 96.f;
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
@@ -103,8 +106,15 @@ __device__ __forceinline__ float sum8(const uint4& v) {
   }
   return s;
 }
-__device__ __forceinline__ uint32_t times2(uint32_t v, uint32_t f) {
-  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v) * __builtin_bit_cast(f16x2, f));
+// A page's scale of values in units of the largest; where there is none, 1.
+__device__ __forceinline__ float in_units(float scale, float unit) { return unit > 0.f ? fmaxf(scale / unit, LEAST_UNITS) : 1.f; }
+// The largest scale of values has grown from `unit` to `now`: what a row's accumulators are to be multiplied by.  Its maximum, which is in these units, goes
+// down with them, so that weights to come are measured by what the row has got so far, as far as its sum (`sum`, of which the lane holds l) stays a number.
+__device__ __forceinline__ float other_unit(float unit, float now, float sum, float& m, float& l) {
+  const float grown = unit > 0.f ? fminf(__builtin_amdgcn_logf(now) - __builtin_amdgcn_logf(unit), 250.f) : 250.f;
+  const float down = fminf(grown, fmaxf(SUM_LOG2 - __builtin_amdgcn_logf(sum), 0.f));
+  m -= down, l *= fast_exp2(down);
+  return unit > 0.f ? fast_exp2(down - grown) : 0.f;
 }
 // Codes that one workgroup reads once: past the caches' order of use.
 __device__ __forceinline__ uint4 once16(const uint8_t* p) {
@@ -229,7 +239,7 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(const CacheAttnArgs
   f32x4 acc[W];
 #pragma unroll
   for (int i = 0; i < W; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = NEG_BIG, l = 0.f, unit = 0.f;  // unit: what the accumulators are to be multiplied by
+  float m = NEG_BIG, l = 0.f, unit = 0.f;  // unit: what the accumulators are to be multiplied by, the largest scale of values so far
   for (int seg = t_lo; seg < t_hi; seg += 64 << pl.page_log2) {
     const int seg_hi = min(t_hi, seg + (64 << pl.page_log2));
     if (seg > t_lo) {
@@ -238,23 +248,24 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(const CacheAttnArgs
       if (seg + wave * 32 < seg_hi) fetch(t0, seg, seg + wave * 32);
     }
     const float unit_now = fmaxf(unit, wave_max(vs));
-    const float again = unit_now > 0.f ? unit / unit_now : 0.f;
-    const uint32_t vr = pack_f16(unit_now > 0.f ? vs / unit_now : 0.f, unit_now > 0.f ? vs / unit_now : 0.f);
-    if (seg > t_lo) {
+    if (unit_now > unit) {
+      if (seg > t_lo) {
+        const float by = other_unit(unit, unit_now, quarter_sum(l), m, l);
 #pragma unroll
-      for (int i = 0; i < W; ++i) acc[i] *= again;
+        for (int i = 0; i < W; ++i) acc[i] *= by;
+      }
+      unit = unit_now;
     }
-    unit = unit_now;
+    const float vf = in_units(vs, unit), lv = __builtin_amdgcn_logf(vf), iv = 1.0f / vf;
     auto use = [&](Tile& x, int t) {
-      float kf[2], p[2][4];
-      uint32_t vf[2];
+      float kf[2], tv[2], ti[2], p[2][4];
       bool ok[2];
       f32x4 z[2];
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const int ts = t + 16 * s, pg = (ts - seg) >> pl.page_log2 & 63;
         ok[s] = lane_int(id, pg) >= 0 && ts < seg_hi;
-        kf[s] = lane_float(ks, pg) * q_scale, vf[s] = (uint32_t)lane_int((int)vr, pg);
+        kf[s] = lane_float(ks, pg) * q_scale, tv[s] = lane_float(lv, pg), ti[s] = lane_float(iv, pg);
         if (KIND == CACHE_E4M3 && (!ok[s] || ts + 16 > seg_hi)) {  // what no token has written may be a NaN
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -276,12 +287,13 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(const CacheAttnArgs
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             z[s][e] = e < left ? z[s][e] * kf[s] : -__builtin_inff();
-            top = fmaxf(top, z[s][e]);
+            top = fmaxf(top, z[s][e] + tv[s]);
           }
           kf[s] = 1.f;
         }
       } else {
-        top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])) * kf[0], fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])) * kf[1]);
+        top = fmaxf(fmaf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), kf[0], tv[0]),
+                    fmaf(fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])), kf[1], tv[1]));
       }
       top = quarter_max(top);
       if (__any(top > m)) {
@@ -291,15 +303,14 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(const CacheAttnArgs
 #pragma unroll
         for (int i = 0; i < W; ++i) acc[i] *= keep;
       }
-      const float off = P_LOG2 - m;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
+        const float off = P_LOG2 - m + tv[s];
 #pragma unroll
         for (int e = 0; e < 4; ++e) p[s][e] = fast_exp2(fmaf(z[s][e], kf[s], off));
-        l += (p[s][0] + p[s][1]) + (p[s][2] + p[s][3]);
+        l = fmaf((p[s][0] + p[s][1]) + (p[s][2] + p[s][3]), ti[s], l);
       }
-      const uint4 pf = make_uint4(times2(pack_f16(p[0][0], p[0][1]), vf[0]), times2(pack_f16(p[0][2], p[0][3]), vf[0]),
-                                  times2(pack_f16(p[1][0], p[1][1]), vf[1]), times2(pack_f16(p[1][2], p[1][3]), vf[1]));
+      const uint4 pf = make_uint4(pack_f16(p[0][0], p[0][1]), pack_f16(p[0][2], p[0][3]), pack_f16(p[1][0], p[1][1]), pack_f16(p[1][2], p[1][3]));
       if (KIND == CACHE_INT8) {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
@@ -384,10 +395,9 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(const CacheAttnArgs
 // next tile's codes are in registers while this one's products run; one barrier a tile.  v_mfma_f32_32x32x16_f16:
 //   S^T[t,i] = K Q^T (lane: query l%32; accumulator rows 8q + 4(l/32) + e),  O^T[d,i] += V^T P^T, P from the accumulators as they are, V^T by transposing
 //   LDS reads.
-// A page's scale of the keys is in the factor of its scores, that of the values, in units of the window's largest one, in the exponent of its
-// weights (their own sum takes it back): neither costs an instruction a score.  Weights are rounded to f16 (11 bits, against the 9 that the result
-// keeps) with a factor of 2^7, so that it holds them down to 2^-31 of the largest; a page whose values are 2^-n of the window's largest
-// loses n of that range, which is an error of 2^-31 of the largest value.  What a window of 512 pages is (id and scales) waits in LDS, too.
+// A page's scale of the keys is in the factor of its scores, that of the values in the exponent of its weights, as above: neither costs an
+// instruction a score.  Weights are rounded to f16 (11 bits, against the 9 that the result keeps) with a factor of 2^7, so that it holds them down to
+// 2^-31 of what the row's largest gives.  What a window of 512 pages is (id and scales) waits in LDS, too.
 // Bound by the vector unit (53 % of the cycles: exponentials, maxima, widening) beside the matrix cores (31 %), two waves a SIMD: 8 prompts of up to
 // 2048 tokens, 32 heads of 128, int8, causal: 138 GFLOP of visible pairs in 215 us, 640 TFLOP/s (the 16-row tiles above: 638 us).
 typedef __attribute__((ext_vector_type(16))) float f32x16;
@@ -449,7 +459,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
   extern __shared__ __attribute__((aligned(256))) uint4 lds[];
   int* const s_id = reinterpret_cast<int*>(lds + 2 * BUF);
   float* const s_ks = reinterpret_cast<float*>(s_id + WINDOW);
-  float* const s_vs = s_ks + WINDOW;  // of values: the scale, then its log2 in units of the window's largest
+  float* const s_vs = s_ks + WINDOW;  // of values: the scale, then its log2 in units of the largest so far
   float* const s_vi = s_vs + WINDOW;  // 2^ less that
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 31, g = lane >> 5;
@@ -536,15 +546,18 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
     float most = unit;
     for (int p = lane; p < n; p += 64) most = fmaxf(most, s_vs[p]);
     most = wave_max(most);
-    const float again = most > 0.f ? unit / most : 0.f;
-    if (unit > 0.f && again != 1.f) {
+    if (most > unit) {
+      if (key > t_lo) {
+        const float2 both = wave_swap32(l);
+        const float by = other_unit(unit, most, both.x + both.y, m, l);
 #pragma unroll
-      for (int i = 0; i < NC; ++i) acc[i] *= again;
+        for (int i = 0; i < NC; ++i) acc[i] *= by;
+      }
+      unit = most;
     }
-    unit = most;
     __syncthreads();  // every wave has read the scales
     for (int p = tid; p < n; p += NT) {
-      const float f = unit > 0.f ? fmaxf(s_vs[p] / unit, 0x1p-40f) : 1.f;  // (2^-40 of the largest is nothing)
+      const float f = in_units(s_vs[p], unit);
       s_vs[p] = __builtin_amdgcn_logf(f), s_vi[p] = 1.0f / f;
     }
     __syncthreads();
@@ -645,12 +658,14 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             const int here = gone >> (2 * sub + x) & 1 ? 0 : left;
+            float most = -__builtin_inff();
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const float z = 16 * (2 * sub + x) + 8 * (e >> 2) + (e & 3) < here ? (s[8 * x + e] + begin) * f[x] : -__builtin_inff();
               s[8 * x + e] = z;
-              top = fmaxf(top, z);
+              most = fmaxf(most, z);
             }
+            top = fmaxf(top, most + now.lv[(2 * sub + x) % NG]);
             f[x] = 1.f;
           }
           start = 0.f;
@@ -660,7 +675,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_prompt_kernel(const CacheAtt
             float most = s[8 * x];
 #pragma unroll
             for (int e = 1; e < 8; ++e) most = fmaxf(most, s[8 * x + e]);
-            top = fmaxf(top, (most + start) * f[x]);
+            top = fmaxf(top, fmaf(most + start, f[x], now.lv[(2 * sub + x) % NG]));
           }
         }
         const float2 both = wave_swap32(top);

@@ -720,3 +720,96 @@ def test_rows_past_the_most_of_a_sequence_are_left_alone(torch, ops, total):
     rest[answered] = False
     assert (o[rest] == 7.0).all() and (lse[rest] == 7.0).all()
     assert torch.isfinite(o[answered]).all() and not (o[answered] == 7.0).all(1).any()
+
+
+def attention_64_by_heads(s, g, q, H, causal, scale, lost=()):
+    """attention_64 for larger calls: the same in products of all rows of a key/value head."""
+    o, lse = np.zeros((s.n_tok, H, s.DH)), np.full((s.n_tok, H), -np.inf)
+    size, reach = np.zeros((s.n_tok, H, s.DH)), np.zeros((s.n_tok, H))
+    share = H // s.HKV
+    for b in range(s.B):
+        T, n = s.total[b], s.new[b]
+        if not T or not n:
+            continue
+        pages = s.table[b, :-(-T // s.page)]
+        there = np.array([(b, t // s.page) not in lost for t in range(T)])
+        seen = np.repeat(there & ((np.arange(T) <= T - n + np.arange(n)[:, None]) if causal else np.ones((n, 1), dtype=bool)), share, axis=0)
+        some = seen.any(1)
+        for h in range(s.HKV):
+            k, v = ((values(p[g][pages, h], s.kind) * sc[g][pages, h].astype(np.float64)[:, None, None]).reshape(-1, s.DH)[:T]
+                    for p, sc in ((s.k, s.ks), (s.v, s.vs)))
+            k, v = np.where(there[:, None], k, 0), np.where(there[:, None], v, 0)
+            at = np.s_[s.ptr[b]:s.ptr[b + 1], h * share:(h + 1) * share]
+            x = q[s.ptr[b]:s.ptr[b + 1]].astype(np.float64).reshape(n, H, s.DH)[:, h * share:(h + 1) * share].reshape(-1, s.DH)
+            z = np.where(seen, x @ k.T * scale, -np.inf)
+            m = np.where(some, z.max(1), 0)
+            p = np.exp(z - m[:, None])
+            total = np.where(some, p.sum(1), 1)
+            far = np.where(seen, np.abs(x) @ np.abs(k).T, 0).max(1) * scale
+            with np.errstate(divide="ignore"):
+                lse[at] = np.where(some, m + np.log(total), -np.inf).reshape(n, share)
+            o[at], size[at] = (p @ v / total[:, None]).reshape(n, share, -1), (p @ np.abs(v) / total[:, None]).reshape(n, share, -1)
+            reach[at] = far.reshape(n, share)
+    return o, lse, size, reach
+
+
+def check_rows_of_one_page_each(torch, ops, kind, DH, page, H, HKV, new, total, step, order, ws=True, slots=5):
+    """Every row has all its weight on the pages of one slot (page number modulo `slots`), whose values are 2^-(step * slot) of the largest: the result is as
+    near to that slot's values as its own size asks, however small they are.  order "grows": the small ones first, over the whole sequence."""
+    s = Setup(torch, ops, kind, 1, HKV, DH, page, new, total, 31)
+    r = np.random.default_rng(32)
+    few = {INT8: 3, E4M3: 8}[kind]                                      # of 127 or 448: what a key has in the other columns
+    for b in range(s.B):
+        n = -(-total[b] // page)
+        for i in range(n):
+            slot = i % slots if order == "any" else (n - 1 - i) * slots // n
+            at = s.table[b, i]
+            x = r.integers(-few, few + 1, size=(HKV, page, DH)).astype(np.float32)
+            x[..., slot] = TOP[kind]
+            s.k[0][at] = to_codes(x, kind)
+            s.v[0][at] = to_codes((r.normal(size=(HKV, page, DH)) * TOP[kind] / 3).astype(np.float32), kind)
+            s.ks[0][at] = np.float32(1) / TOP[kind]
+            s.vs[0][at] = np.float32(0.01 * 2.0 ** (-step * slot)) * r.uniform(0.7, 1.4, HKV).astype(np.float32)
+    for pools, scales, k, sc in ((s.pools[0], s.scales[0], s.k, s.ks), (s.pools[1], s.scales[1], s.v, s.vs)):
+        pools[0].copy_(s.dev(k[0]))
+        scales[0].copy_(s.dev(sc[0]))
+    x = r.normal(size=(s.n_tok, H, DH)) * 0.05
+    row = np.arange(s.n_tok)[:, None] + np.arange(H)[None]
+    np.put_along_axis(x, (row % slots)[..., None], 40.0, axis=-1)
+    q = bf16(x.reshape(s.n_tok, -1))
+    which = {n: s.call[n] for n in ("n_tok", "max_q", "max_len")}
+    size = ops.hydra_op_cache_attention_ws_bytes(s.cache, H, **which) if ws else 0
+    scratch = [torch.full((size,), 0xff, dtype=torch.uint8, device="cuda")] if size else None
+    o, lse = torch.full((s.n_tok, H * DH), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((s.n_tok, H), 7.0, device="cuda")
+    ops.hydra_op_cache_attention(s.cache, s.lens, H, H * DH, H * DH, False, 1.0, [s.dev(q).to(torch.bfloat16)], [o], [lse], ws=scratch, **s.call)
+    want, want_lse, mag, reach = attention_64_by_heads(s, 0, q, H, False, 1.0)
+    got, got_lse = o.float().cpu().numpy().reshape(s.n_tok, H, DH).astype(np.float64), lse.cpu().numpy().astype(np.float64)
+    e = reach * (DH + 8) * 2.0 ** -24 + 2.0 ** -20                      # as in check_attention
+    off = np.abs(got - want) / (2.0 ** -8 * np.abs(want) + mag * (2.0 ** -10 + 2 * e[..., None]) + 1e-30)
+    assert off.max() <= 1, (off.max(), [float(off[row % slots == i].max()) for i in range(slots)])
+    assert np.all(np.abs(got_lse - want_lse) <= 2 * e + 2.0 ** -20 * (8 + np.abs(want_lse)))
+
+
+@pytest.mark.parametrize("kind", [INT8, E4M3])
+@pytest.mark.parametrize("order", ["any", "grows"])
+@pytest.mark.parametrize("step", [5, 10, 15])
+@pytest.mark.parametrize("DH,page,total", [(64, 16, 400), (128, 64, 330), (128, 16, 1500)])
+def test_attention_of_tokens_that_see_small_values_alone(torch, ops, kind, order, step, DH, page, total):
+    check_rows_of_one_page_each(torch, ops, kind, DH, page, 10, 2, [1, 3], [total, total - 7], step, order)
+
+
+@pytest.mark.parametrize("kind", [INT8, E4M3])
+@pytest.mark.parametrize("order", ["any", "grows"])
+@pytest.mark.parametrize("step", [5, 10, 15])
+@pytest.mark.parametrize("DH,page", [(64, 16), (128, 64)])
+def test_attention_of_prompts_that_see_small_values_alone(torch, ops, kind, order, step, DH, page):
+    check_rows_of_one_page_each(torch, ops, kind, DH, page, 60, 12, [150, 100], [330, 320], step, order)
+
+
+@pytest.mark.parametrize("kind", [INT8, E4M3])
+@pytest.mark.parametrize("order", ["any", "grows"])
+@pytest.mark.parametrize("step", [5, 10, 15])
+def test_attention_of_small_values_alone_in_one_run_of_many_pages(torch, ops, kind, order, step):
+    """Without scratch a run is all of a sequence: more pages than the kernels know at a time (64; 512 for prompts), the largest values among the last."""
+    check_rows_of_one_page_each(torch, ops, kind, 128, 16, 10, 2, [2, 1], [3000, 1900], step, order, ws=False)
+    check_rows_of_one_page_each(torch, ops, kind, 64, 16, 60, 12, [20], [18000], step, order, ws=False)
