@@ -215,6 +215,9 @@ typedef struct {
 } hydra_cache_attention_desc;
 int hydra_op_cache_attention(const hydra_cache_attention_desc* d, void* stream);
 size_t hydra_op_cache_attention_ws_bytes(const hydra_cache_desc* cache, int H);
+/* How a call of these sizes with enough scratch is launched: plan = {rows of a key/value head that one workgroup has, its waves, runs that a sequence's
+ * tokens are split into}.  16 rows: the kernel for few rows, more: the one for prompts. */
+int hydra_op_cache_attention_plan(const hydra_cache_desc* cache, int H, int32_t plan[3]);
 
 /* One token per row of logits_g [rows, ldz] (fp32 or bf16, V columns, 262144 at most), drawn from given uniforms u_g [rows, ldu] in [0, 1), one per token.
  * temperature, top_k, top_p, min_p: device arrays of `rows` entries, shared by the group.  With tokens in order of falling logits (the lower index

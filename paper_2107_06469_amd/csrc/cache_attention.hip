@@ -906,6 +906,11 @@ size_t cache_attn_ws_bytes(const CacheArgs& c, int H) {
   return p.n_split == 1 ? 0 : ((size_t)c.n_tok * H * p.n_split * (c.DH + 2) * sizeof(float) + 15) / 16 * 16;
 }
 
+void cache_attn_plan(const CacheArgs& c, int H, int32_t plan[3]) {
+  const CacheAttnPlan p = plan_of(c, H);
+  plan[0] = p.prompt ? p.waves * 32 : 16, plan[1] = p.waves, plan[2] = p.n_split;
+}
+
 const char* cache_attn_sizes_refusal(const CacheArgs& c, int H) {
   if (const char* why = cache_sizes_refusal(c)) return why;
   if (H < 1 || H % c.HKV) return "H is no multiple of HKV";

@@ -332,6 +332,7 @@ const char* cache_sizes_refusal(const CacheArgs& c);  // the part that needs no 
 const char* cache_attn_sizes_refusal(const CacheArgs& c, int H);
 const char* cache_attn_refusal(const CacheAttnArgs& a);
 size_t cache_attn_ws_bytes(const CacheArgs& c, int H);
+void cache_attn_plan(const CacheArgs& c, int H, int32_t plan[3]);  // rows and waves of a workgroup, runs of keys
 hipError_t cache_attn_init();
 hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t s);
 

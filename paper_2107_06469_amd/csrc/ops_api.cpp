@@ -290,6 +290,14 @@ size_t hydra_op_cache_attention_ws_bytes(const hydra_cache_desc* d, int H) {
   return cache_attn_sizes_refusal(c, H) ? 0 : cache_attn_ws_bytes(c, H);
 }
 
+int hydra_op_cache_attention_plan(const hydra_cache_desc* d, int H, int32_t plan[3]) {
+  if (!cache_tables(d) || !plan) return bad("hydra_op_cache_attention_plan: NULL table or G out of range");
+  const CacheArgs c = cache_args(d);
+  if (const char* why = cache_attn_sizes_refusal(c, H)) return ops_fail(HYDRA_ERR_INVALID_ARG, "hydra_op_cache_attention_plan", why);
+  cache_attn_plan(c, H, plan);
+  return HYDRA_OK;
+}
+
 int hydra_op_cache_attention(const hydra_cache_attention_desc* d, void* stream) {
   if (!d || !cache_tables(&d->cache) || !d->q || !d->o) return bad("hydra_op_cache_attention: NULL table or G out of range");
   CacheAttnArgs a{};

@@ -64,6 +64,7 @@ def _L():
         L.hydra_op_cache_attention.argtypes = [vp, vp]
         L.hydra_op_cache_attention_ws_bytes.argtypes = [vp, C.c_int]
         L.hydra_op_cache_attention_ws_bytes.restype = C.c_size_t
+        L.hydra_op_cache_attention_plan.argtypes = [vp, C.c_int, vp]
         L.hydra_op_sample.argtypes = [C.c_int] * 6 + [pp, pp, vp, vp, vp, vp, pp, pp, vp]
         L.hydra_op_empty_launches.argtypes = [C.c_int, vp]
         L.hydra_ops_last_error.restype = C.c_char_p
@@ -286,6 +287,13 @@ def hydra_op_cache_append(cache, lens, H, ld_qkv, ld_q, qkv, q=None, *, rot=ROT_
 
 def hydra_op_cache_attention_ws_bytes(cache, H, *, n_tok=None, max_q=1, max_len=None) -> int:
     return int(_L().hydra_op_cache_attention_ws_bytes(_cache_desc(*cache.fields(n_tok=n_tok, max_q=max_q, max_len=max_len)), H))
+
+
+def hydra_op_cache_attention_plan(cache, H, *, n_tok=None, max_q=1, max_len=None):
+    """(rows of a workgroup, its waves, runs of a sequence's tokens) of a call with enough scratch; 16 rows: the kernel for few rows."""
+    plan = (C.c_int32 * 3)()
+    _check(_L().hydra_op_cache_attention_plan(_cache_desc(*cache.fields(n_tok=n_tok, max_q=max_q, max_len=max_len)), H, plan))
+    return tuple(plan)
 
 
 def hydra_op_cache_attention(cache, lens, H, ld_q, ld_o, causal, scale, q, o, lse=None, *, ws=None, q_ptr=None, n_tok=None, max_q=1, max_len=None):

@@ -200,3 +200,22 @@ def test_draws_are_checked(bad, monkeypatch):
     token = [torch.zeros(3, dtype=torch.int64 if bad == "token64" else torch.int32)] * n("token")
     with pytest.raises(ValueError):
         ops.hydra_op_sample(ops.F32, 3, 50, 50, 50, z, z[:n("u")], *rule.values(), token, [torch.zeros(3)] * n("logprob"))
+
+
+def test_which_kernel_takes_a_call():
+    """The kernel for few rows or the one for prompts, its waves and the runs of keys, at sizes that tests of either count on."""
+    def plan(G, HKV, DH, new, total, H):
+        d, keep = cache(G=G, B=len(new), HKV=HKV, DH=DH, page=16, n_tok=sum(new), max_q=max(new), max_len=max(total), max_pages=-(-max(total) // 16))
+        out = (C.c_int32 * 3)()
+        assert ops._L().hydra_op_cache_attention_plan(ops._cache_desc(*d), H, out) == 0
+        return tuple(out)
+    assert plan(1, 2, 64, [1, 3], [400, 393], 10)[0] == 16 and plan(1, 2, 128, [1, 3], [1500, 1493], 10) == (16, 8, 6)
+    assert plan(1, 2, 128, [2, 1], [3000, 1900], 10)[0] == 16                          # in one run without scratch: more than 64 pages
+    assert plan(1, 12, 64, [150, 100], [330, 320], 60)[:2] == plan(1, 12, 128, [150, 100], [330, 320], 60)[:2] == (128, 4)
+    assert plan(1, 12, 64, [20], [18000], 60)[:2] == (128, 4)                          # more than 512
+    assert plan(3, 8, 128, [200, 0, 131], [230, 50, 131], 16) == (128, 4, 1)
+    assert plan(2, 4, 128, [40, 33, 0, 7], [1500, 1411, 20, 1300], 36)[:2] == (256, 8) and plan(2, 4, 128, [40, 33], [1500, 1411], 36)[0] == 16
+    out = (C.c_int32 * 3)()
+    assert ops._L().hydra_op_cache_attention_plan(None, 4, out) == 1 and ops._L().hydra_op_cache_attention_plan(ops._cache_desc(*cache(DH=96)[0]), 4, out) == 1
+    d, keep = cache()
+    assert ops._L().hydra_op_cache_attention_plan(ops._cache_desc(*d), 4, None) == 1

@@ -722,10 +722,11 @@ def test_rows_past_the_most_of_a_sequence_are_left_alone(torch, ops, total):
     assert torch.isfinite(o[answered]).all() and not (o[answered] == 7.0).all(1).any()
 
 
-def attention_64_by_heads(s, g, q, H, causal, scale, lost=()):
-    """attention_64 for larger calls: the same in products of all rows of a key/value head."""
+def attention_64_by_heads(s, g, q, H, causal, scale, lost=(), most=False):
+    """attention_64 for larger calls: the same in products of all rows of a key/value head.  most: and the row's largest weight times its page's scale of
+    values."""
     o, lse = np.zeros((s.n_tok, H, s.DH)), np.full((s.n_tok, H), -np.inf)
-    size, reach = np.zeros((s.n_tok, H, s.DH)), np.zeros((s.n_tok, H))
+    size, reach, largest = np.zeros((s.n_tok, H, s.DH)), np.zeros((s.n_tok, H)), np.zeros((s.n_tok, H))
     share = H // s.HKV
     for b in range(s.B):
         T, n = s.total[b], s.new[b]
@@ -750,7 +751,9 @@ def attention_64_by_heads(s, g, q, H, causal, scale, lost=()):
                 lse[at] = np.where(some, m + np.log(total), -np.inf).reshape(n, share)
             o[at], size[at] = (p @ v / total[:, None]).reshape(n, share, -1), (p @ np.abs(v) / total[:, None]).reshape(n, share, -1)
             reach[at] = far.reshape(n, share)
-    return o, lse, size, reach
+            if most:
+                largest[at] = ((p * np.repeat(s.vs[g][pages, h].astype(np.float64), s.page)[:T]).max(1) / total).reshape(n, share)
+    return (o, lse, size, reach, largest) if most else (o, lse, size, reach)
 
 
 def check_rows_of_one_page_each(torch, ops, kind, DH, page, H, HKV, new, total, step, order, ws=True, slots=5):
@@ -813,3 +816,154 @@ def test_attention_of_small_values_alone_in_one_run_of_many_pages(torch, ops, ki
     """Without scratch a run is all of a sequence: more pages than the kernels know at a time (64; 512 for prompts), the largest values among the last."""
     check_rows_of_one_page_each(torch, ops, kind, 128, 16, 10, 2, [2, 1], [3000, 1900], step, order, ws=False)
     check_rows_of_one_page_each(torch, ops, kind, 64, 16, 60, 12, [20], [18000], step, order, ws=False)
+
+
+# ---- the kernel for prompts, in every form ----------------------------------------------------------------------------
+
+
+def check_prompts(torch, ops, s, H, causal, rows, split, ws=True, in_place=False, pad=0, lost=(), scale=0.05, n_tok=None):
+    """A call that the kernel for prompts takes with `rows` rows to a workgroup, in several runs of keys or one, against 64 bits.  Tolerances: those of
+    check_attention, and what f16 has below its normal numbers.  Weights are held as w_t = 2^7 p_t v_t / (at most the largest p v of the row), p the weight, v the
+    page's scale of values; below 2^-14 f16 rounds them to 2^-25, so that T keys of codes up to the kind's largest are off by T 2^-32 times that code times the
+    row's largest p v.  It tells in columns alone in which the keys that the row looks at have the code 0."""
+    n_tok = n_tok or s.n_tok
+    call = dict(s.call, n_tok=n_tok)
+    which = {n: call[n] for n in ("n_tok", "max_q", "max_len")}
+    plan = ops.hydra_op_cache_attention_plan(s.cache, H, **which)
+    assert plan[:2] == (rows, rows // 32), plan
+    size = ops.hydra_op_cache_attention_ws_bytes(s.cache, H, **which) if ws else 0
+    assert ((plan[2] > 1) if ws else False) == (size > 0) == split, (plan, size)
+    scratch = [torch.full((size,), 0xff, dtype=torch.uint8, device="cuda") for _ in range(s.G)] if size else None
+    host, q = zip(*(s.bf16(n_tok, H * s.DH + pad) for _ in range(s.G)))
+    q = [x.clone() for x in q]
+    o = q if in_place else [torch.full((n_tok, H * s.DH + pad), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(s.G)]
+    lse = [torch.full((n_tok, H), 7.0, device="cuda") for _ in range(s.G)]
+    ops.hydra_op_cache_attention(s.cache, s.lens, H, H * s.DH + pad, H * s.DH + pad, causal, scale, q, o, lse, ws=scratch, **call)
+    torch.cuda.synchronize()
+    for g in range(s.G):
+        want, want_lse, mag, reach, most = attention_64_by_heads(s, g, host[g][:s.n_tok, :H * s.DH], H, causal, scale, lost=lost, most=True)
+        least = max(s.total) * 2.0 ** -32 * float(TOP[s.kind]) * most[..., None]
+        got = o[g].float().cpu().numpy()
+        assert in_place or (got[s.n_tok:] == 7.0).all() and (got[:, H * s.DH:] == 7.0).all() and bool((lse[g][s.n_tok:] == 7.0).all())
+        got = got[:s.n_tok, :H * s.DH].reshape(s.n_tok, H, s.DH).astype(np.float64)
+        e = reach * (s.DH + 8) * 2.0 ** -24 + 2.0 ** -20
+        off = np.abs(got - want) / (2.0 ** -8 * np.abs(want) + mag * (2.0 ** -10 + 2 * e[..., None]) + least + 1e-30)
+        assert off.max() <= 1, (g, off.max(), np.unravel_index(off.argmax(), off.shape))
+        got_lse, empty = lse[g][:s.n_tok].cpu().numpy().astype(np.float64), np.isneginf(want_lse)
+        assert np.array_equal(np.isneginf(got_lse), empty) and np.all(got[empty] == 0)
+        assert np.all((np.abs(got_lse[~empty] - want_lse[~empty]) <= (2 * e + 2.0 ** -20 * (8 + np.abs(want_lse)))[~empty]))
+
+
+@pytest.mark.parametrize("kind", [INT8, E4M3])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("DH,page", [(128, 64), (128, 16), (64, 32), (64, 128)])
+def test_prompts_of_a_group(torch, ops, kind, causal, DH, page):
+    """Three models, four waves, one run; sequences without tokens in the call, and without any."""
+    s = Setup(torch, ops, kind, 3, 8, DH, page, [200, 0, 131, 0, 77], [230, 50, 131, 0, 300], 41, spare=64)
+    check_prompts(torch, ops, s, 16, causal, 128, False, pad=8)
+
+
+@pytest.mark.parametrize("kind,DH,page,causal", [(INT8, 128, 64, True), (E4M3, 128, 16, True), (E4M3, 64, 64, False), (INT8, 64, 16, True)])
+def test_prompts_in_several_runs(torch, ops, kind, DH, page, causal):
+    """Four waves, few blocks of rows behind many keys, two models: joined; the second sequence ends inside the first run."""
+    s = Setup(torch, ops, kind, 2, 2, DH, page, [500, 130], [3000, 133], 42)
+    check_prompts(torch, ops, s, 2, causal, 128, True)
+    check_prompts(torch, ops, s, 2, causal, 128, False, ws=False)
+    check_prompts(torch, ops, s, 2, causal, 128, True, n_tok=s.n_tok + 3)     # rows of no sequence
+
+
+@pytest.mark.parametrize("kind,page,causal", [(INT8, 64, True), (E4M3, 64, False), (E4M3, 16, True), (INT8, 32, False)])
+def test_prompts_by_eight_waves(torch, ops, kind, page, causal):
+    """Blocks of 256 rows: few rows behind many keys, two models, in one run (without scratch) and in several."""
+    s = Setup(torch, ops, kind, 2, 4, 128, page, [40, 33, 0, 7], [1500, 1411, 20, 1300], 43)
+    check_prompts(torch, ops, s, 36, causal, 256, True)
+    check_prompts(torch, ops, s, 36, causal, 256, False, ws=False)
+
+
+@pytest.mark.parametrize("kind,causal", [(INT8, True), (E4M3, False)])
+@pytest.mark.parametrize("H,rows", [(132, 128), (528, 256)])
+def test_prompts_over_more_pages_than_are_known_at_a_time(torch, ops, kind, causal, H, rows):
+    """A run of more than 512 pages of 16 tokens (without scratch), and the largest values among the last."""
+    s = Setup(torch, ops, kind, 2, 2, 128, 16, [1, 1, 1, 1], [20000, 8193, 8192, 16390], 44)
+    for g in range(2):
+        for b in range(4):
+            s.vs[g][s.table[b, 512:-(-s.total[b] // 16)]] *= 300.0
+        s.scales[1][g].copy_(s.dev(s.vs[g]))
+    check_prompts(torch, ops, s, H, causal, rows, False, ws=False)
+    check_prompts(torch, ops, s, H, causal, rows, True)
+
+
+@pytest.mark.parametrize("kind", [INT8, E4M3])
+@pytest.mark.parametrize("page", [16, 64, 128])
+@pytest.mark.parametrize("split", [True, False])
+def test_prompts_with_pages_that_are_not_there(torch, ops, kind, page, split):
+    s = Setup(torch, ops, kind, 1, 12, 128, page, [150, 150, 100], [1100, 300, 151], 45)
+    lost = {(0, 0), (1, 1), (0, 1000 // page), (2, 0)} | ({(0, 40), (0, 41), (0, 42), (0, 43), (1, 5)} if page == 16 else set())
+    for n, (b, p) in enumerate(sorted(lost)):
+        s.table[b, p] = (-1, s.n_pages, 1 << 30)[n % 3]
+    s.cache = ops.Cache(kind, *s.pools, *s.scales, s.dev(s.table))
+    s.table = np.clip(s.table, 0, s.n_pages - 1)
+    check_prompts(torch, ops, s, 60, True, 128, split, ws=split, lost=lost)
+
+
+@pytest.mark.parametrize("kind,DH", [(INT8, 128), (E4M3, 64)])
+def test_prompts_in_place_and_rows_that_see_nothing(torch, ops, kind, DH):
+    s = Setup(torch, ops, kind, 2, 8, DH, 32, [190, 200, 150], [95, 203, 150], 46)     # the first one's first 95 rows lie before its first token
+    check_prompts(torch, ops, s, 24, True, 128, False, in_place=True)
+    check_prompts(torch, ops, s, 24, True, 128, False, pad=16)
+    s = Setup(torch, ops, kind, 1, 3, DH, 64, [300, 20], [2300, 10], 47)
+    check_prompts(torch, ops, s, 15, True, 128, True, in_place=True)
+
+
+def test_prompts_with_more_rows_than_a_sequence_may_have(torch, ops):
+    for total, split in ((400, False), (3000, True)):
+        s = Setup(torch, ops, INT8, 1, 8 if split else 24, 64, 32, [160, 0, 200], [total, 30, total], 48)
+        H, most, n = 4 * s.HKV, 150, s.n_tok
+        call = dict(s.call, max_q=most)
+        which = {k: call[k] for k in ("n_tok", "max_q", "max_len")}
+        plan = ops.hydra_op_cache_attention_plan(s.cache, H, **which)
+        assert plan[0] == 128 and (plan[2] > 1) == split, plan
+        ws = [torch.full((ops.hydra_op_cache_attention_ws_bytes(s.cache, H, **which),), 0xff, dtype=torch.uint8, device="cuda")] if split else None
+        q = torch.randn(n, H * 64, device="cuda").to(torch.bfloat16)
+        o = torch.full_like(q, 7.0)
+        ops.hydra_op_cache_attention(s.cache, s.lens, H, H * 64, H * 64, True, 0.125, [q], [o], ws=ws, **call)
+        assert (o[150:160] == 7.0).all() and (o[310:] == 7.0).all()
+        for part in (o[:150], o[160:310]):
+            assert torch.isfinite(part).all() and not (part == 7.0).all(1).any()
+
+
+@pytest.mark.parametrize("kind", [INT8, E4M3])
+def test_prompts_over_a_cache_of_zeros_and_queries_of_all_sizes(torch, ops, kind):
+    s = Setup(torch, ops, kind, 1, 8, 64, 32, [300, 290], [300, 290], 49)
+    H, n = 32, s.n_tok
+    assert ops.hydra_op_cache_attention_plan(s.cache, H, **{k: s.call[k] for k in ("n_tok", "max_q", "max_len")})[0] == 128
+    x, q = s.bf16(n, H * 64)
+    got = []
+    for by in (1.0, 2.0 ** -100, 2.0 ** 90):
+        o, lse = torch.empty_like(q), torch.empty((n, H), device="cuda")
+        ops.hydra_op_cache_attention(s.cache, s.lens, H, H * 64, H * 64, True, 0.05 / by, [q * by], [o], [lse], **s.call)
+        got.append((o.float(), lse))
+    for o, lse in got[1:]:
+        assert float((o - got[0][0]).abs().max()) < 0.02 * float(got[0][0].abs().max()) and float((lse - got[0][1]).abs().max()) < 1e-4
+    zeros = torch.zeros((n, (H + 16) * 64), dtype=torch.bfloat16, device="cuda")
+    o, lse = torch.ones((n, H * 64), dtype=torch.bfloat16, device="cuda"), torch.empty((n, H), device="cuda")
+    ops.hydra_op_cache_append(s.cache, s.lens, H, (H + 16) * 64, 0, [zeros], None, **s.call)
+    ops.hydra_op_cache_attention(s.cache, s.lens, H, (H + 16) * 64, H * 64, True, 0.1, [zeros], [o], [lse], **s.call)
+    want = torch.log(torch.cat([torch.arange(1, m + 1, device="cuda") for m in s.new]).double())[:, None]
+    assert bool((o == 0).all()) and float((lse.double() - want).abs().max()) < 2.0 ** -19
+
+
+@pytest.mark.parametrize("n,total,rows", [(170, 1300, 128), (140, 1300, 256)])
+def test_prompts_over_pages_past_32_bits(torch, ops, n, total, rows):
+    """Pages more than 4 GiB into a pool of 5.2 GB."""
+    s = Setup(torch, ops, INT8, 1, 8, 128, 128, [n], [total], 50)
+    at = np.array([39999, 3, 39000, 35001, 2, 37777, 33000, 39998, 0, 36000, 34567])
+    pools = [[torch.zeros((40000, 8, 128, 128), dtype=torch.int8, device="cuda")] for _ in range(2)]
+    scales = [[torch.full((40000, 8), 0.01, device="cuda")] for _ in range(2)]
+    there = torch.from_numpy(at).cuda()
+    for pool, scale, host, sc in zip(pools, scales, (s.k, s.v), (s.ks, s.vs)):
+        pool[0][there] = s.dev(host[0][s.table[0]].view(np.int8))
+        scale[0][there] = s.dev(sc[0][s.table[0]])
+    s.cache = ops.Cache(INT8, *pools, *scales, s.dev(at[None].astype(np.int32)))
+    check_prompts(torch, ops, s, 64, True, rows, True)
+    check_prompts(torch, ops, s, 64, True, rows, False, ws=False)
