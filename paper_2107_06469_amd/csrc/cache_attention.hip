@@ -15,8 +15,8 @@
 // what a page gives to the row, however small the values of the pages that the row looks at (down to 2^-64 of the largest; smaller scales
 // count as that).  Maxima, sums, scores and accumulators are fp32.
 //
-// Bound by HBM where there are keys to read, 2 DH bytes each and head: 2 x 64 sequences of up to 2048 tokens over 8 heads of 128 (406 MB) in 75 us,
-// 5.4 TB/s, where the loads alone of this kernel take 70; 8 of up to 32768 (385 MB) in 71.  One sequence of 513 tokens takes 9, nearly all of it
+// Bound by HBM where there are keys to read, 2 DH bytes each and head: 2 x 64 sequences of up to 2048 tokens over 8 heads of 128 (406 MB) in 76 us,
+// 5.3 TB/s, where the loads alone of this kernel take 70; 8 of up to 32768 (385 MB) in 72.  One sequence of 513 tokens takes 9, nearly all of it
 // latency: lengths and pages, codes, the join of the waves.
 #include <algorithm>
 #include <type_traits>
@@ -398,8 +398,9 @@ __global__ __launch_bounds__(NW * 64) void cache_attn_kernel(const CacheAttnArgs
 // A page's scale of the keys is in the factor of its scores, that of the values in the exponent of its weights, as above: neither costs an
 // instruction a score.  Weights are rounded to f16 (11 bits, against the 9 that the result keeps) with a factor of 2^7, so that it holds them down to
 // 2^-31 of what the row's largest gives.  What a window of 512 pages is (id and scales) waits in LDS, too.
-// Bound by the vector unit (53 % of the cycles: exponentials, maxima, widening) beside the matrix cores (31 %), two waves a SIMD: 8 prompts of up to
-// 2048 tokens, 32 heads of 128, int8, causal: 138 GFLOP of visible pairs in 215 us, 640 TFLOP/s (the 16-row tiles above: 638 us).
+// 8 prompts of up to 2048 tokens, 32 heads of 128, int8, causal: 138 GFLOP of visible pairs in 209 us back to back, 660 TFLOP/s (from an idle chip 240; the
+// 16-row tiles above: 638).  Bound by the chain product, maximum, exponential, product of each half tile, which two waves a SIMD do not cover: the vector
+// unit works for 53 % of the cycles (exponentials, maxima, widening), the matrix cores for 32 %, both for 13 % of them, neither for 28 %.
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 __device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);

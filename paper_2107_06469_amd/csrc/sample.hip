@@ -14,8 +14,8 @@
 // Where the list's tokens are known without the histogram it is left out: those that min_p leaves, and for a small top_k those at or above the top_k-th of
 // the threads' largest logits.
 // Bound by one CU's vector unit, each instruction a token being 2048 cycles of 131072 tokens, and LDS atomics, for many rows: 256 of 131072 in bf16
-// with top-p and min-p 34 us, 2.0 TB/s; 2 x 64 of 32000 in fp32 with mixed rules 34, of which a row with a top-k of 1500 and top-p takes 27.  A
-// single row of 32000 with a top-k of 50 and top-p takes 13, a chain of passes and barriers.  With the histogram for these too, the 256 rows take 142 and the single
+// with top-p and min-p 35 us, 1.9 TB/s (50 to 60 where the smallest min-p leaves more than the list holds); 2 x 64 of 32000 in fp32 with mixed rules 35,
+// of which a row with a top-k of 1500 and top-p takes 27.  A single row of 32000 with a top-k of 50 and top-p takes 13, a chain of passes and barriers.  With the histogram for these too, the 256 rows take 142 and the single
 // one 17.  Rows that do not fit LDS are read again, through the caches.  A kept set larger than the list costs another pass, over the uniforms
 // too (131072 tokens, top-p 0.97 alone: 115 us).
 #include <float.h>
